@@ -36,6 +36,7 @@ enum {
     Q8T_ERR_BITS = -3,      /* bit width outside [2,16] (or not 8 / 16 where fixed) */
     Q8T_ERR_OVERFLOW = -4,  /* reduction length too large for the 32-bit accumulator contract */
     Q8T_ERR_WORKSPACE = -5, /* ws is NULL or misaligned although the call needs one */
+    Q8T_ERR_VALUE = -7,     /* a type, format or factor that is not among the allowed ones */
     Q8T_ERR_HIP = -6        /* a launch was rejected by the runtime */
 };
 
@@ -435,6 +436,83 @@ int q8t_relu_bwd_add(const float *g, const float *out, const float *other, int64
 int q8t_relu_bwd_sum(const float *g1, const float *g2, const float *out, int64_t n, float *res, void *stream);
 int q8t_relu_bwd_sum_lattice(const float *g1, const float *g2s, const float *out, int N, int C, int H, int W, int stride,
                              float *res, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * The 8-bit layer step of a language model (not from the paper).  A transformer's activations hold a few channels that are
+ * far larger than the others, so one range a tensor is too coarse for them; codes are 8-bit floating point there, with a scale
+ * for every 128 entries along the axis that a product sums over, and the normalization runs along a token's row.
+ *
+ * Types of float tensors: Q8T_F32, Q8T_BF16.  All arithmetic is fp32 and a result is rounded to its type once.  Row-major,
+ * contiguous; any alignment of the type itself.  step (nullable): a device counter that is added to the seed, so that a
+ * captured graph draws anew at every replay.  Q8T_ERR_VALUE: a type, format or factor outside the allowed ones.  Outputs may
+ * not overlap inputs unless it is said below. */
+enum { Q8T_F32 = 0, Q8T_BF16 = 1 };
+enum { Q8T_E4M3 = 0, Q8T_E5M2 = 1 };
+
+/* Codes of x [rows, cols] in 8-bit floating point (e4m3: largest 448, NaN, no infinities; e5m2: largest 57344, infinities and
+ * NaN) with a power of two as scale of each block of 128:
+ *   E = the smallest whole number with  max |x_i| over the block's finite entries <= (448 | 57344) * 2^E,  in [-127, 127]; 0 for
+ *       a block without a finite entry other than 0
+ *   code_i = x_i / 2^E rounded to the format: to nearest even, or (stochastic != 0) the magnitude in steps u of the code's last
+ *       place to floor(u) + [frac(u)*65536 > r + 0.5] with r the 16 bits of the generator of q8t_quantize for (seed + step, flat
+ *       index of x_i).  An infinity becomes NaN in e4m3.
+ * Blocks: 1 x 128 along the rows for q and 128 x 1 down the columns for qt, or (square != 0) 128 x 128, where both copies hold the
+ * same values.
+ *   q  [rows][128*ceil(cols/128)]: codes, filled up with zeros;  s  [rows][4*ceil(cols/512)]: E + 127 of each block, filled up with 127
+ *   qt [cols][128*ceil(rows/128)], st [cols][4*ceil(rows/512)]: the transposed copy, nullable (both).  q, qt 16-byte aligned.
+ * rows or cols may be 0 (nothing is written).  rows*cols <= 2^34, rows*ceil(cols/128) and cols*ceil(rows/128) < 2^28.
+ * Errors: Q8T_ERR_SHAPE (sizes, alignment), Q8T_ERR_VALUE, Q8T_ERR_NULL, Q8T_ERR_HIP. */
+int q8t_fp8_quantize(const void *x, int type, int64_t rows, int64_t cols, int format, int square, int stochastic, uint64_t seed,
+                     const int64_t *step, uint8_t *q, uint8_t *s, uint8_t *qt, uint8_t *st, void *stream);
+
+/* out[m][n] = sum_k A[m][k] B[n][k] over codes as q8t_fp8_quantize leaves them: a [M][128*ceil(K/128)], sa [M][4*ceil(K/512)], b and sb
+ * likewise with N rows.  A fp32 result is summed in fp32; for a bf16 result the products are added in groups of eight, where what lies
+ * below 2^-13 of the group's largest product is lost, and the groups in fp32.  What a code and its scale stand for has to be within
+ * the range of fp32, as it is where it came from there.  The three products of a layer Y[M,N] = X[M,K] W[K,N]:
+ *   forward          a = q of X,  b = qt of W          layer gradient   a = q of dY,  b = q of W
+ *   weight gradient  a = qt of X, b = qt of dY
+ * out: [M][N], Q8T_F32 or Q8T_BF16.  a, b 16-byte, sa, sb 4-byte aligned.  M or N may be 0 (nothing is written).
+ * ws: q8t_fp8_gemm_workspace_size(M, N, K) bytes (may be 0), 16-byte aligned.  A row whose codes or scales hold a NaN gives NaN in
+ * its row (column) of the result and nowhere else.
+ * Errors: Q8T_ERR_SHAPE (sizes, alignment), Q8T_ERR_VALUE, Q8T_ERR_NULL, Q8T_ERR_WORKSPACE, Q8T_ERR_HIP. */
+size_t q8t_fp8_gemm_workspace_size(int M, int N, int K);
+int q8t_fp8_gemm(const uint8_t *a, const uint8_t *sa, int format_a, const uint8_t *b, const uint8_t *sb, int format_b, int M, int N, int K,
+                 void *out, int type, void *ws, void *stream);
+
+/* The end of one block and the start of the next, for each of T rows of D entries (1 <= D <= 16384, T < 2^22):
+ *   u = h / sqrt(mean(h^2) + eps) * w_post                      the norm behind the block (w_post NULL: u = h)
+ *   res_out = res_scale * res + branch_scale * drop(gate * u)   the residual stream
+ *   y = res_out / sqrt(mean(res_out^2) + eps) * w_pre           the norm in front of the next block (w_pre NULL: none)
+ * drop(v) = v / (1 - p) where a position is kept, else 0: see q8t_dropout for p, seed and step; p = 0 keeps everything.
+ * res, h, res_out, y [T][D] of one type; w_post, w_pre [D] floats; gate [groups][D] of the same type, row g for the rows
+ * [g*T/groups, (g+1)*T/groups): 1 for a gate per channel, the number of sequences, or T for one per token (gate NULL: groups = 0,
+ * no gate).  h NULL: the norm in front alone, over res (no w_post, gate, p; res_scale 1; res_out is not written).
+ * y: values of the type, and / or q [T][128*ceil(D/128)], s [T][4*ceil(D/512)]: its e4m3 codes as q8t_fp8_quantize(y in fp32, square = 0)
+ * would give them; with w_pre at least one, else none.  y follows from the stream before it is rounded to the type of res_out.
+ * stats (nullable): [2][T] floats, 1 / sqrt(..) of the two norms (1 without w_post; row 0 not written without h, row 1 without
+ * w_pre), kept for the backward pass.  res_out may be res or h; q 16-byte aligned.  T may be 0. */
+int q8t_residual_norm_fwd(const void *res, const void *h, const float *w_post, const void *gate, int64_t groups, const float *w_pre, int type,
+                          int64_t T, int D, float eps, float res_scale, float branch_scale, double p, uint64_t seed, const int64_t *step,
+                          void *res_out, void *y, float *stats, uint8_t *q, uint8_t *s, void *stream);
+
+/* Backward of the above.  dy: gradient with respect to y (NULL without w_pre); dres_out (nullable: 0): with respect to res_out from
+ * its other consumers; res_out and stats as the forward call left them (without h: res_out is res).
+ * Outputs: dres [T][D] (nullable with h), dh [T][D] (with h), dgate [groups][D] of the tensors' type (with a gate), dw_post, dw_pre
+ * [D] floats (with the weights).  Sums over rows are taken in one order whatever runs beside them.  dres may be dy or dres_out.  T may
+ * be 0: the sums are then 0.  ws: q8t_residual_norm_bwd_workspace_size(T, D, groups) bytes, 16-byte aligned.
+ * Errors of both: Q8T_ERR_SHAPE, Q8T_ERR_VALUE, Q8T_ERR_NULL (also for an output without its input), Q8T_ERR_WORKSPACE, Q8T_ERR_HIP. */
+size_t q8t_residual_norm_bwd_workspace_size(int64_t T, int D, int64_t groups);
+int q8t_residual_norm_bwd(const void *dy, const void *dres_out, const void *res_out, const void *h, const float *stats, const float *w_post,
+                          const void *gate, int64_t groups, const float *w_pre, int type, int64_t T, int D, float res_scale,
+                          float branch_scale, double p, uint64_t seed, const int64_t *step, void *dres, void *dh, void *dgate,
+                          float *dw_post, float *dw_pre, void *ws, void *stream);
+
+/* out_i = (residual ? residual_i : 0) + (kept_i ? x_i / (1 - p') : 0) over n elements; position i is kept iff its 16 bits of the generator
+ * of q8t_quantize for (seed + step, i) are at least cut = round(65536 p), p' = cut / 65536; 0 <= p <= 1.  The mask is stored nowhere: the
+ * gradient of x is the same call on the gradient of out (without the residual).  x where it is not kept has no effect, whatever its
+ * value.  out may be x or residual.  n <= 2^34.  Errors: Q8T_ERR_SHAPE, Q8T_ERR_VALUE, Q8T_ERR_NULL, Q8T_ERR_HIP. */
+int q8t_dropout(const void *x, const void *residual, int type, int64_t n, double p, uint64_t seed, const int64_t *step, void *out,
+                void *stream);
 
 /* Measurement aid, not a step of the method: a plain streaming kernel of known traffic with the access
  * shape of the library's HBM-bound calls (every workgroup streams one contiguous slice, four 16-byte

@@ -22,7 +22,7 @@ _lib = C.CDLL(LIB_PATH)
 from . import _q8t_calls as _calls  # noqa: E402  (linked against the library)
 
 ERRORS = {-1: "Q8T_ERR_NULL", -2: "Q8T_ERR_SHAPE", -3: "Q8T_ERR_BITS", -4: "Q8T_ERR_OVERFLOW",
-          -5: "Q8T_ERR_WORKSPACE", -6: "Q8T_ERR_HIP"}
+          -5: "Q8T_ERR_WORKSPACE", -6: "Q8T_ERR_HIP", -7: "Q8T_ERR_VALUE"}
 
 
 class Q8TError(RuntimeError):
@@ -45,7 +45,7 @@ class ConvDesc(C.Structure):
 
 
 QPARAMS_BYTES = 24
-_vp, _i, _i64, _u64, _f, _sz = C.c_void_p, C.c_int, C.c_int64, C.c_uint64, C.c_float, C.c_size_t
+_vp, _i, _i64, _u64, _f, _d, _sz = C.c_void_p, C.c_int, C.c_int64, C.c_uint64, C.c_float, C.c_double, C.c_size_t
 
 _SIGS = {
     "q8t_quantize_workspace_size": (_sz, [_i64]),
@@ -111,6 +111,13 @@ _SIGS = {
     "q8t_xnor_gemm": (_i, [_vp, _vp, _i, _i, _i, _vp, _vp]),
     "q8t_tern_wgrad_multi_workspace_size": (_sz, [_i, _i, _i]),
     "q8t_tern_wgrad_multi": (_i, [_vp, _vp, _i, _i, _i, _i, _u64, _vp, _vp, _vp, _vp]),
+    "q8t_fp8_quantize": (_i, [_vp, _i, _i64, _i64, _i, _i, _i, _u64] + [_vp] * 6),
+    "q8t_fp8_gemm_workspace_size": (_sz, [_i, _i, _i]),
+    "q8t_fp8_gemm": (_i, [_vp, _vp, _i, _vp, _vp, _i, _i, _i, _i, _vp, _i, _vp, _vp]),
+    "q8t_residual_norm_fwd": (_i, [_vp] * 4 + [_i64, _vp, _i, _i64, _i, _f, _f, _f, _d, _u64] + [_vp] * 7),
+    "q8t_residual_norm_bwd_workspace_size": (_sz, [_i64, _i, _i64]),
+    "q8t_residual_norm_bwd": (_i, [_vp] * 7 + [_i64, _vp, _i, _i64, _i, _f, _f, _d, _u64] + [_vp] * 8),
+    "q8t_dropout": (_i, [_vp, _vp, _i, _i64, _d, _u64, _vp, _vp, _vp]),
     "q8t_range_bn_scale": (C.c_double, [_i64]),
     "q8t_version": (C.c_char_p, []),
 }
@@ -610,3 +617,53 @@ def relu_bwd_add(g, out, other=None):
     res = torch.empty_like(g)
     _check(_lib.q8t_relu_bwd_add(_ptr(g), _ptr(out), _ptr(other), g.numel(), _ptr(res), _stream()), "q8t_relu_bwd_add")
     return res
+
+
+# ------------------------------------------------------------------ the 8-bit layer step of a language model
+# float tensors of float32 or bfloat16, contiguous, all of a call on one device; the call runs there, on that device's current stream.
+# step: None, or a device tensor of one int64 that is added to the seed (a captured graph then draws anew at every replay).
+_FORMATS = {"e4m3": 0, "e5m2": 1}
+_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _one_of(table, key, what):
+    if key not in table:
+        raise ValueError("q8t: %s is one of %s" % (what, ", ".join(str(k) for k in table)))
+    return table[key]
+
+
+def fp8_quantize(x, fmt="e4m3", square=False, stochastic=False, seed=0, step=None, transposed=False, q_out=None, s_out=None, qt_out=None,
+                 st_out=None):
+    """Codes of a matrix [R, C] in 8-bit floating point ("e4m3", "e5m2") with a power of two as scale of every 128 entries of a row,
+    or of every 128 x 128 block (square).  Returns (q, s, qt, st): q [R, C filled up to 128] codes and s [R, one a block, filled up to a
+    multiple of 4] scales (float8_e8m0fnu); with transposed=True the copy whose blocks run down the columns as well, qt [C, R filled
+    up to 128] and st, else None."""
+    return _calls.fp8_quantize(x, _one_of(_FORMATS, fmt, "fmt"), square, stochastic, seed, step, transposed, q_out, s_out, qt_out, st_out)
+
+
+def fp8_gemm(a, sa, b, sb, dtype=torch.bfloat16, out=None, ws=None):
+    """[M, N] = A [M, K] B [N, K]^T over codes and scales of fp8_quantize, sums in fp32; dtype: float32 or bfloat16.  With Y = X W:
+    forward (q of X, qt of W), layer gradient (q of dY, q of W), weight gradient (qt of X, qt of dY)."""
+    return _calls.fp8_gemm(a, sa, b, sb, _one_of(_TYPES, dtype, "dtype"), out, ws)
+
+
+def residual_norm_fwd(res, h=None, w_post=None, gate=None, w_pre=None, eps=1e-6, res_scale=1.0, branch_scale=1.0, p=0.0, seed=0, step=None,
+                      quantized=False, want_y=True):
+    """res_out = res_scale*res + branch_scale*drop(gate * rmsnorm(h)*w_post), y = rmsnorm(res_out)*w_pre over the rows of res [..., D]
+    (w_post None: h as it is; gate [groups, D]; w_pre None: no y; h None: y = rmsnorm(res)*w_pre alone).
+    Returns (res_out, y, stats[2, T], q, s), None where not asked for; quantized: q, s = the e4m3 codes and scales of y."""
+    return _calls.residual_norm_fwd(res, h, w_post, gate, w_pre, eps, res_scale, branch_scale, p, seed, step, quantized, want_y)
+
+
+def residual_norm_bwd(dy, dres_out, res_out, h, stats, w_post=None, gate=None, w_pre=None, res_scale=1.0, branch_scale=1.0, p=0.0, seed=0,
+                      step=None, ws=None):
+    """Gradients of residual_norm_fwd from those of y (None without w_pre) and of res_out's other consumers (or None); the other
+    arguments as in the forward call, res_out and stats as it returned them (h None: res_out is res).
+    Returns (dres, dh, dgate, dw_post, dw_pre), None where the forward call had no such input."""
+    return _calls.residual_norm_bwd(dy, dres_out, res_out, h, stats, w_post, gate, w_pre, res_scale, branch_scale, p, seed, step, ws)
+
+
+def dropout(x, p, seed=0, step=None, residual=None, out=None):
+    """[residual +] x / (1 - p) where the generator's 16 bits for (seed + step, flat position) keep it, else 0 (p in steps of 2^-16).
+    The gradient of x: the same call on the gradient of the result, without the residual."""
+    return _calls.dropout(x, p, seed, step, residual, out)

@@ -1,0 +1,54 @@
+// Drop-out with a mask that is never stored: the 16 bits of the library's counter-based generator for (seed + step, flat
+// position) decide whether a position is kept, so the backward pass draws the same mask again from the same arguments.
+//   out_i = residual_i + (kept_i ? x_i * scale : 0),   scale = 1 / (1 - cut / 65536): unbiased exactly
+// A position that is not kept takes nothing of x: an infinity or a NaN there does not reach the result.
+#include "typed_rows.h"
+
+namespace {
+
+constexpr int kThreads = 256, kPer = 8;
+
+template <class T, bool RES>
+__global__ __launch_bounds__(kThreads) void dropout_kernel(const T *__restrict__ x, const T *res, int64_t n, Q8tDrop d, uint64_t seed,
+                                                           const int64_t *__restrict__ step, T *out)
+{
+    const Q8tSeed s = q8t_seed(seed, step);
+    const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kPer;
+    if (i >= n) return;
+    const int count = n - i >= kPer ? kPer : (int)(n - i);
+    float v[kPer], r[kPer];
+    uint32_t bits[kPer];
+    q8t_load8(x + i, v, count);
+    if (RES) q8t_load8(res + i, r, count);
+    q8t_draw8<true>(i, s, bits);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const float y = bits[k] >= d.cut ? v[k] * d.scale : 0.0f;
+        v[k] = RES ? r[k] + y : y;
+    }
+    q8t_store8(out + i, v, count);
+}
+
+template <class T>
+int launch(const void *x, const void *res, int64_t n, const Q8tDrop &d, uint64_t seed, const int64_t *step, void *out, hipStream_t st)
+{
+    const dim3 grid((unsigned)((n + kThreads * kPer - 1) / (kThreads * kPer)));
+    if (res) dropout_kernel<T, true><<<grid, kThreads, 0, st>>>((const T *)x, (const T *)res, n, d, seed, step, (T *)out);
+    else dropout_kernel<T, false><<<grid, kThreads, 0, st>>>((const T *)x, nullptr, n, d, seed, step, (T *)out);
+    Q8T_LAUNCH_CHECK();
+    return Q8T_OK;
+}
+
+}  // namespace
+
+extern "C" int q8t_dropout(const void *x, const void *residual, int type, int64_t n, double p, uint64_t seed, const int64_t *step,
+                           void *out, void *stream)
+{
+    Q8tDrop d;
+    if (n < 0 || n > ((int64_t)1 << 34)) return Q8T_ERR_SHAPE;
+    if ((type != Q8T_F32 && type != Q8T_BF16) || !q8t_drop(p, &d)) return Q8T_ERR_VALUE;
+    if (n == 0) return Q8T_OK;
+    if (!x || !out) return Q8T_ERR_NULL;
+    return type == Q8T_F32 ? launch<float>(x, residual, n, d, seed, step, out, (hipStream_t)stream)
+                           : launch<q8t_bf16>(x, residual, n, d, seed, step, out, (hipStream_t)stream);
+}

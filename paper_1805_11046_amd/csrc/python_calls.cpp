@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -560,6 +561,211 @@ PyObject *range_bn_add_relu_quantize(Argv a)
     return results({&out, &q, &p});
 }
 
+// ---- the 8-bit layer step of a language model ----
+// Its calls run on the device of their first tensor, on that device's current stream, and refuse tensors of another device.
+typedef c10::OptionalDeviceGuard Here;
+
+const at::Tensor &beside(PyObject *o, const at::Tensor &first)
+{
+    const at::Tensor &t = dev(o);
+    if (t.device() != first.device()) raise(PyExc_ValueError, "q8t: all tensors of a call are on one device");
+    return t;
+}
+void is(const at::Tensor &t, at::IntArrayRef shape, at::ScalarType type, const char *what)
+{
+    if (t.scalar_type() != type || !t.sizes().equals(shape)) raise(PyExc_ValueError, what);
+}
+// a tensor of this shape and type on the device of `first`, or none
+at::Tensor maybe(PyObject *o, const at::Tensor &first, at::IntArrayRef shape, at::ScalarType type, const char *what)
+{
+    if (o == Py_None) return at::Tensor();
+    const at::Tensor &t = beside(o, first);
+    is(t, shape, type, what);
+    return t;
+}
+at::Tensor result(PyObject *o, const at::Tensor &first, at::IntArrayRef shape, at::ScalarType type, const char *what)
+{
+    return o == Py_None ? make(shape, type, first) : maybe(o, first, shape, type, what);
+}
+int float_type(const at::Tensor &t)
+{
+    if (t.scalar_type() == at::kFloat) return Q8T_F32;
+    if (t.scalar_type() == at::kBFloat16) return Q8T_BF16;
+    raise(PyExc_ValueError, "q8t: a tensor of float32 or bfloat16 is expected");
+}
+int code_format(const at::Tensor &t)
+{
+    if (t.scalar_type() == at::kFloat8_e4m3fn) return Q8T_E4M3;
+    if (t.scalar_type() == at::kFloat8_e5m2) return Q8T_E5M2;
+    raise(PyExc_ValueError, "q8t: codes of float8_e4m3fn or float8_e5m2 are expected");
+}
+double wide(PyObject *o)   // float(o)
+{
+    const Ref f(PyNumber_Float(o));
+    return PyFloat_AS_DOUBLE(f.o);
+}
+const int64_t *counter(PyObject *o, const at::Tensor &first)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = beside(o, first);
+    if (t.scalar_type() != at::kLong || t.numel() != 1) raise(PyExc_ValueError, "q8t: step is a tensor of one int64");
+    return ptr<int64_t>(t);
+}
+int64_t code_bytes(int64_t n) { return (n + 127) / 128 * 128; }
+int64_t scale_bytes(int64_t n) { return (n + 511) / 512 * 4; }
+
+// x, format, square, stochastic, seed, step, transposed, q_out, s_out, qt_out, st_out
+PyObject *fp8_quantize(Argv a)
+{
+    const at::Tensor &x = dev(a[0]);
+    const Here here(x.device());
+    if (x.dim() != 2) raise(PyExc_ValueError, "q8t: a matrix is expected");
+    const int64_t R = x.size(0), C = x.size(1);
+    const int type = float_type(x), format = integer(a[1]), square = truth(a[2]), stochastic = truth(a[3]);
+    const uint64_t s0 = seed(a[4]);
+    const int64_t *step = counter(a[5], x);
+    const at::ScalarType code = format == Q8T_E4M3 ? at::kFloat8_e4m3fn : at::kFloat8_e5m2;
+    const char *what = "q8t: an output has another shape or type than the codes or scales";
+    const at::Tensor q = result(a[7], x, {R, code_bytes(C)}, code, what);
+    const at::Tensor s = result(a[8], x, {R, scale_bytes(C)}, at::kFloat8_e8m0fnu, what);
+    at::Tensor qt, st;
+    if (truth(a[6])) {
+        qt = result(a[9], x, {C, code_bytes(R)}, code, what);
+        st = result(a[10], x, {C, scale_bytes(R)}, at::kFloat8_e8m0fnu, what);
+    }
+    run("q8t_fp8_quantize", [&](void *stream) {
+        return q8t_fp8_quantize(ptr<void>(x), type, R, C, format, square, stochastic, s0, step, ptr<uint8_t>(q), ptr<uint8_t>(s),
+                                ptr<uint8_t>(qt), ptr<uint8_t>(st), stream);
+    });
+    return results({&q, &s, &qt, &st});
+}
+
+// a, sa, b, sb, type, out, ws
+PyObject *fp8_gemm(Argv v)
+{
+    const at::Tensor &a = dev(v[0]);
+    const Here here(a.device());
+    const at::Tensor &sa = beside(v[1], a), &b = beside(v[2], a), &sb = beside(v[3], a);
+    if (a.dim() != 2 || b.dim() != 2) raise(PyExc_ValueError, "q8t: matrices are expected");
+    const int fa = code_format(a), fb = code_format(b), type = integer(v[4]);
+    const int64_t K = a.size(1);
+    if (K % 128 || b.size(1) != K) raise(PyExc_ValueError, "q8t: rows of codes are whole blocks of 128 and alike in both operands");
+    const char *what = "q8t: scales are one float8_e8m0fnu a block of 128, a multiple of 4 in a row";
+    is(sa, {a.size(0), scale_bytes(K)}, at::kFloat8_e8m0fnu, what);
+    is(sb, {b.size(0), scale_bytes(K)}, at::kFloat8_e8m0fnu, what);
+    const int M = Plane::dim(a.size(0)), N = Plane::dim(b.size(0)), k = Plane::dim(K);
+    const at::Tensor out = result(v[5], a, {M, N}, type == Q8T_F32 ? at::kFloat : at::kBFloat16, "q8t: out has another shape or type than the result");
+    const Scratch ws(v[6], q8t_fp8_gemm_workspace_size(M, N, k), v[0], true);
+    run("q8t_fp8_gemm", [&, w = ws.get()](void *stream) {
+        return q8t_fp8_gemm(ptr<uint8_t>(a), ptr<uint8_t>(sa), fa, ptr<uint8_t>(b), ptr<uint8_t>(sb), fb, M, N, k, ptr<void>(out), type, w, stream);
+    });
+    return wrap(out);
+}
+
+struct Rows {   // T rows of D entries
+    int64_t T;
+    int D;
+    explicit Rows(const at::Tensor &t)
+    {
+        if (t.dim() < 1 || t.size(-1) < 1) raise(PyExc_ValueError, "q8t: a tensor of rows is expected");
+        D = Plane::dim(t.size(-1));
+        T = t.numel() / D;
+    }
+};
+int64_t gate_rows(PyObject *gate)
+{
+    if (gate == Py_None) return 0;
+    const at::Tensor &t = tensor(gate);
+    if (t.dim() != 2 || t.size(0) < 1) raise(PyExc_ValueError, "q8t: a gate of [groups, D] is expected");
+    return t.size(0);
+}
+
+// res, h, w_post, gate, w_pre, eps, res_scale, branch_scale, p, seed, step, quantized, want_y
+PyObject *residual_norm_fwd(Argv a)
+{
+    const at::Tensor &res = dev(a[0]);
+    const Here here(res.device());
+    const Rows n(res);
+    const int type = float_type(res);
+    const at::ScalarType t = res.scalar_type();
+    const int64_t groups = gate_rows(a[3]);
+    const at::Tensor h = maybe(a[1], res, res.sizes(), t, "q8t: h has another shape or type than res");
+    const at::Tensor w_post = maybe(a[2], res, {n.D}, at::kFloat, "q8t: w_post is one float32 a column");
+    const at::Tensor gate = maybe(a[3], res, {groups, n.D}, t, "q8t: the gate has another width or type than res");
+    const at::Tensor w_pre = maybe(a[4], res, {n.D}, at::kFloat, "q8t: w_pre is one float32 a column");
+    const float eps = real(a[5]), res_scale = real(a[6]), branch_scale = real(a[7]);
+    const double p = wide(a[8]);
+    const uint64_t s0 = seed(a[9]);
+    const int64_t *step = counter(a[10], res);
+    const bool pre = w_pre.defined(), quantized = pre && truth(a[11]);
+    at::Tensor res_out, y, q, s;
+    if (h.defined()) res_out = same(res);
+    if (pre && (truth(a[12]) || !quantized)) y = same(res);
+    const at::Tensor stats = make({2, n.T}, at::kFloat, res);
+    if (quantized) {
+        q = make({n.T, code_bytes(n.D)}, at::kFloat8_e4m3fn, res);
+        s = make({n.T, scale_bytes(n.D)}, at::kFloat8_e8m0fnu, res);
+    }
+    run("q8t_residual_norm_fwd", [&](void *stream) {
+        return q8t_residual_norm_fwd(ptr<void>(res), ptr<void>(h), ptr<float>(w_post), ptr<void>(gate), groups, ptr<float>(w_pre), type, n.T, n.D,
+                                     eps, res_scale, branch_scale, p, s0, step, ptr<void>(res_out), ptr<void>(y), ptr<float>(stats),
+                                     ptr<uint8_t>(q), ptr<uint8_t>(s), stream);
+    });
+    return results({&res_out, &y, &stats, &q, &s});
+}
+
+// dy, dres_out, res_out, h, stats, w_post, gate, w_pre, res_scale, branch_scale, p, seed, step, ws
+PyObject *residual_norm_bwd(Argv a)
+{
+    const at::Tensor &r = dev(a[2]);
+    const Here here(r.device());
+    const Rows n(r);
+    const int type = float_type(r);
+    const at::ScalarType t = r.scalar_type();
+    const int64_t groups = gate_rows(a[6]);
+    const at::Tensor dy = maybe(a[0], r, r.sizes(), t, "q8t: dy has another shape or type than res_out");
+    const at::Tensor dres_out = maybe(a[1], r, r.sizes(), t, "q8t: dres_out has another shape or type than res_out");
+    const at::Tensor h = maybe(a[3], r, r.sizes(), t, "q8t: h has another shape or type than res_out");
+    const at::Tensor stats = maybe(a[4], r, {2, n.T}, at::kFloat, "q8t: stats are those of the forward call");
+    const at::Tensor w_post = maybe(a[5], r, {n.D}, at::kFloat, "q8t: w_post is one float32 a column");
+    const at::Tensor gate = maybe(a[6], r, {groups, n.D}, t, "q8t: the gate has another width or type than res_out");
+    const at::Tensor w_pre = maybe(a[7], r, {n.D}, at::kFloat, "q8t: w_pre is one float32 a column");
+    const float res_scale = real(a[8]), branch_scale = real(a[9]);
+    const double p = wide(a[10]);
+    const uint64_t s0 = seed(a[11]);
+    const int64_t *step = counter(a[12], r);
+    at::Tensor dh, dgate, dw_post, dw_pre;
+    const at::Tensor dres = same(r);
+    if (h.defined()) dh = same(r);
+    if (gate.defined()) dgate = same(gate);
+    if (w_post.defined()) dw_post = make({n.D}, at::kFloat, r);
+    if (w_pre.defined()) dw_pre = make({n.D}, at::kFloat, r);
+    const Scratch ws(a[13], q8t_residual_norm_bwd_workspace_size(n.T, n.D, groups), a[2]);
+    run("q8t_residual_norm_bwd", [&, w = ws.get()](void *stream) {
+        return q8t_residual_norm_bwd(ptr<void>(dy), ptr<void>(dres_out), ptr<void>(r), ptr<void>(h), ptr<float>(stats), ptr<float>(w_post),
+                                     ptr<void>(gate), groups, ptr<float>(w_pre), type, n.T, n.D, res_scale, branch_scale, p, s0, step,
+                                     ptr<void>(dres), ptr<void>(dh), ptr<void>(dgate), ptr<float>(dw_post), ptr<float>(dw_pre), w, stream);
+    });
+    return results({&dres, &dh, &dgate, &dw_post, &dw_pre});
+}
+
+// x, p, seed, step, residual, out
+PyObject *dropout(Argv a)
+{
+    const at::Tensor &x = dev(a[0]);
+    const Here here(x.device());
+    const int type = float_type(x);
+    const double p = wide(a[1]);
+    const uint64_t s0 = seed(a[2]);
+    const int64_t *step = counter(a[3], x);
+    const at::Tensor res = maybe(a[4], x, x.sizes(), x.scalar_type(), "q8t: the residual has another shape or type than x");
+    const at::Tensor out = result(a[5], x, x.sizes(), x.scalar_type(), "q8t: out has another shape or type than x");
+    run("q8t_dropout", [&](void *stream) {
+        return q8t_dropout(ptr<void>(x), ptr<void>(res), type, x.numel(), p, s0, step, ptr<void>(out), stream);
+    });
+    return wrap(out);
+}
+
 template <PyObject *(*F)(Argv), int N>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -612,6 +818,11 @@ PyMethodDef methods[] = {
     CALL("range_bn_bwd_bifurcate", range_bn_bwd_bifurcate<false>, 17),
     CALL("range_bn_relu_bwd_bifurcate", range_bn_bwd_bifurcate<true>, 17),
     CALL("range_bn_add_relu_quantize", range_bn_add_relu_quantize, 10),
+    CALL("fp8_quantize", fp8_quantize, 11),
+    CALL("fp8_gemm", fp8_gemm, 7),
+    CALL("residual_norm_fwd", residual_norm_fwd, 13),
+    CALL("residual_norm_bwd", residual_norm_bwd, 14),
+    CALL("dropout", dropout, 6),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_q8t_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
