@@ -127,7 +127,7 @@ def test_quantize_beyond_32_bits():
 # ---------------------------------------------------------------------------------------- products
 PRODUCTS = [(1, 1, 1), (1, 16, 128), (1, 4096, 512), (1, 1000, 4100), (2, 17, 129), (16, 48, 640), (17, 33, 1000), (5, 300, 2049), (33, 1, 700),
             (64, 64, 128), (65, 127, 384), (128, 128, 512), (200, 1000, 515), (129, 257, 1025), (256, 256, 256), (255, 513, 130), (300, 520, 4097),
-            (513, 1030, 260), (640, 768, 1536), (1, 20, 16384), (24, 40, 16500), (128, 256, 8200)]
+            (513, 1030, 260), (640, 768, 1536), (1, 20, 16384), (24, 40, 16500), (128, 256, 8200), (1000, 1100, 700), (2000, 2100, 390), (4200, 4100, 140), (70, 300, 8192)]
 
 
 def _operand(R, K, fmt, seed, whole=False):

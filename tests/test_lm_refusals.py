@@ -33,7 +33,7 @@ def test_fp8_gemm(L):
         return L.q8t_fp8_gemm(a, sa, fa, b, sb, fb, M, N, K, out, type, None, None)
     assert all(f(**{k: None}) == NULL for k in ("a", "sa", "b", "sb", "out"))
     assert f(fa=2) == VALUE and f(fb=-1) == VALUE and f(type=2) == VALUE
-    assert f(M=-1) == SHAPE and f(N=-1) == SHAPE and f(K=0) == SHAPE and f(K=-5) == SHAPE and f(K=(1 << 30) + 1) == SHAPE and f(M=(1 << 22) + 1) == SHAPE
+    assert f(M=-1) == SHAPE and f(N=-1) == SHAPE and f(K=0) == SHAPE and f(K=-5) == SHAPE and f(K=(1 << 23) + 1) == SHAPE and f(M=1 << 19, N=(1 << 17) + 1) == SHAPE and f(M=(1 << 22) + 1) == SHAPE
     assert f(a=8) == SHAPE and f(b=8) == SHAPE and f(sa=2) == SHAPE and f(sb=2) == SHAPE
     assert f(M=0, a=None, out=None) == 0 and f(N=0) == 0
     assert L.q8t_fp8_gemm_workspace_size(0, 4, 4) == 0 and L.q8t_fp8_gemm_workspace_size(-1, 4, 4) == 0
