@@ -497,7 +497,7 @@ int q8t_residual_norm_fwd(const void *res, const void *h, const float *w_post, c
 
 /* Backward of the above.  dy: gradient with respect to y (NULL without w_pre); dres_out (nullable: 0): with respect to res_out from
  * its other consumers; res_out and stats as the forward call left them (without h: res_out is res).
- * Outputs: dres [T][D] (nullable with h), dh [T][D] (with h), dgate [groups][D] of the tensors' type (with a gate), dw_post, dw_pre
+ * Outputs: dres [T][D], dh [T][D] (with h), dgate [groups][D] of the tensors' type (with a gate), dw_post, dw_pre
  * [D] floats (with the weights).  Sums over rows are taken in one order whatever runs beside them.  dres may be dy or dres_out.  T may
  * be 0: the sums are then 0.  ws: q8t_residual_norm_bwd_workspace_size(T, D, groups) bytes, 16-byte aligned.
  * Errors of both: Q8T_ERR_SHAPE, Q8T_ERR_VALUE, Q8T_ERR_NULL (also for an output without its input), Q8T_ERR_WORKSPACE, Q8T_ERR_HIP. */

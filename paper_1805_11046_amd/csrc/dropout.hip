@@ -8,7 +8,7 @@ namespace {
 
 constexpr int kThreads = 256, kPer = 8;
 
-template <class T, bool RES>
+template <class T, bool RES, bool ALL>   // ALL: everything is kept
 __global__ __launch_bounds__(kThreads) void dropout_kernel(const T *__restrict__ x, const T *res, int64_t n, Q8tDrop d, uint64_t seed,
                                                            const int64_t *__restrict__ step, T *out)
 {
@@ -17,24 +17,24 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(const T *__restrict__
     if (i >= n) return;
     const int count = n - i >= kPer ? kPer : (int)(n - i);
     float v[kPer], r[kPer];
-    uint32_t bits[kPer];
+    uint32_t bits[4];
     q8t_load8(x + i, v, count);
     if (RES) q8t_load8(res + i, r, count);
-    q8t_draw8<true>(i, s, bits);
+    if (!ALL) q8t_draw8<true>(i, s, bits);
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-        const float y = bits[k] >= d.cut ? v[k] * d.scale : 0.0f;
+        const float y = ALL ? v[k] : (q8t_kept(bits, k, d.below) ? v[k] * d.scale : 0.0f);
         v[k] = RES ? r[k] + y : y;
     }
-    q8t_store8(out + i, v, count);
+    q8t_store8<true>(out + i, v, count);
 }
 
-template <class T>
+template <class T, bool RES>
 int launch(const void *x, const void *res, int64_t n, const Q8tDrop &d, uint64_t seed, const int64_t *step, void *out, hipStream_t st)
 {
     const dim3 grid((unsigned)((n + kThreads * kPer - 1) / (kThreads * kPer)));
-    if (res) dropout_kernel<T, true><<<grid, kThreads, 0, st>>>((const T *)x, (const T *)res, n, d, seed, step, (T *)out);
-    else dropout_kernel<T, false><<<grid, kThreads, 0, st>>>((const T *)x, nullptr, n, d, seed, step, (T *)out);
+    if (d.cut) dropout_kernel<T, RES, false><<<grid, kThreads, 0, st>>>((const T *)x, (const T *)res, n, d, seed, step, (T *)out);
+    else dropout_kernel<T, RES, true><<<grid, kThreads, 0, st>>>((const T *)x, (const T *)res, n, d, seed, step, (T *)out);
     Q8T_LAUNCH_CHECK();
     return Q8T_OK;
 }
@@ -49,6 +49,8 @@ extern "C" int q8t_dropout(const void *x, const void *residual, int type, int64_
     if ((type != Q8T_F32 && type != Q8T_BF16) || !q8t_drop(p, &d)) return Q8T_ERR_VALUE;
     if (n == 0) return Q8T_OK;
     if (!x || !out) return Q8T_ERR_NULL;
-    return type == Q8T_F32 ? launch<float>(x, residual, n, d, seed, step, out, (hipStream_t)stream)
-                           : launch<q8t_bf16>(x, residual, n, d, seed, step, out, (hipStream_t)stream);
+    hipStream_t st = (hipStream_t)stream;
+    if (type == Q8T_F32)
+        return residual ? launch<float, true>(x, residual, n, d, seed, step, out, st) : launch<float, false>(x, nullptr, n, d, seed, step, out, st);
+    return residual ? launch<q8t_bf16, true>(x, residual, n, d, seed, step, out, st) : launch<q8t_bf16, false>(x, nullptr, n, d, seed, step, out, st);
 }

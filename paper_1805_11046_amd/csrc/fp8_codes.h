@@ -57,7 +57,7 @@ __device__ __forceinline__ uint32_t fp8_stochastic(float t, uint32_t r16)
 
 // 8 codes of values v under the stored scale
 template <int FMT, bool STOCH>
-__device__ __forceinline__ uint2 fp8_codes8(const float v[8], uint32_t scale, const uint32_t r[8])
+__device__ __forceinline__ uint2 fp8_codes8(const float v[8], uint32_t scale, const uint32_t r[4])
 {
     const float inv = fp8_inverse(scale);
     uint32_t w[2];
@@ -70,7 +70,7 @@ __device__ __forceinline__ uint2 fp8_codes8(const float v[8], uint32_t scale, co
         } else {
             w[h] = 0u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[h] |= fp8_stochastic<FMT>(p[i] * inv, r[4 * h + i]) << (8 * i);
+            for (int i = 0; i < 4; ++i) w[h] |= fp8_stochastic<FMT>(p[i] * inv, q8t_draw(r, 4 * h + i)) << (8 * i);
         }
     }
     return make_uint2(w[0], w[1]);

@@ -476,9 +476,9 @@ __global__ __launch_bounds__(256) void fold_slices(const float *__restrict__ par
     if (i >= n) return;
     const int count = n - i >= 8 ? 8 : (int)(n - i);
     float v[8], w[8];
-    q8t_load8_kept(part + i, v, count);
+    q8t_load8<float, false>(part + i, v, count);
     for (int z = 1; z < slices; ++z) {
-        q8t_load8_kept(part + z * n + i, w, count);
+        q8t_load8<float, false>(part + z * n + i, w, count);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] += w[k];
     }

@@ -17,7 +17,7 @@ __global__ __launch_bounds__(kThreads) void quantize_rows(const T *__restrict__ 
     const int64_t c = (int64_t)kb * 128 + lane * 8, at = (int64_t)row * C + c;
     const int64_t left = C - c;
     float v[8];
-    uint32_t r[8];
+    uint32_t r[4];
     q8t_load8(x + at, v, left >= 8 ? 8 : (int)left);
     if (STOCH) q8t_draw8<ALIGNED>(at, q8t_seed(seed, step), r);
     const uint32_t scale = fp8_scale<FMT>(fp8_max16(fp8_max8(v)));
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void quantize_tile(const T *__restrict__ 
     for (int j = 0; j < 8; ++j) patch[j] = make_uint2(0u, 0u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        uint32_t r[8];
+        uint32_t r[4];
         if (STOCH) q8t_draw8<ALIGNED>((r0 + i) * C + c0, sd, r);
         const uint32_t scale = fp8_scale<FMT>(rmax[i]);
         const uint2 w = fp8_codes8<FMT, STOCH>(v[i], scale, r);
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kThreads) void quantize_tile(const T *__restrict__ 
             uint32_t code[8];
             if (STOCH) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) code[j] = fp8_stochastic<FMT>(v[i][j] * fp8_inverse(fp8_scale<FMT>(cmax[j])), r[j]);
+                for (int j = 0; j < 8; ++j) code[j] = fp8_stochastic<FMT>(v[i][j] * fp8_inverse(fp8_scale<FMT>(cmax[j])), q8t_draw(r, j));
                 t.x = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
                 t.y = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
             } else {

@@ -64,9 +64,11 @@ def test_residual_norm(L):
 @pytest.mark.parametrize("T,groups", [(T, G) for T in (1, 2, 511, 512, 513, 1000, 1024, 1536, 4100, 100000) for G in (0, 1, 2, 3, 5, 7, 500, 512, T)
                                       if G == 0 or T % G == 0])
 def test_workspace_of_the_norms_backward_stays_small(L, T, groups):
-    # at most about twice 512 workgroups leave their sums behind, and a workgroup has at least one row
-    chunks = L.q8t_residual_norm_bwd_workspace_size(T, 8, groups) / (3 * 8 * 4)
-    assert 1 <= chunks <= min(1100, 2 * T)
+    # a workgroup a chunk of rows leaves three rows of sums (whole lines): at most about twice 2048 chunks of narrow rows, 512 of wide
+    # ones, of one row at least
+    for D, most in ((8, 2048), (4096, 512)):
+        chunks = L.q8t_residual_norm_bwd_workspace_size(T, D, groups) / (3 * max(D, 32) * 4)
+        assert 1 <= chunks <= min(2.2 * most, 2 * T)
 
 
 def test_dropout(L):
