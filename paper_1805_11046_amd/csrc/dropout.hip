@@ -9,7 +9,7 @@ namespace {
 constexpr int kThreads = 256, kPer = 8;
 
 template <class T, bool RES, bool ALL>   // ALL: everything is kept
-__global__ __launch_bounds__(kThreads) void dropout_kernel(const T *__restrict__ x, const T *res, int64_t n, Q8tDrop d, uint64_t seed,
+__global__ __launch_bounds__(kThreads) void dropout_kernel(const T *x, const T *res, int64_t n, Q8tDrop d, uint64_t seed,
                                                            const int64_t *__restrict__ step, T *out)
 {
     const Q8tSeed s = q8t_seed(seed, step);

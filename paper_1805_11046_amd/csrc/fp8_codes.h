@@ -40,19 +40,46 @@ __device__ __forceinline__ uint32_t fp8_pack2(float a, float b, uint32_t old)
                                       : __builtin_amdgcn_cvt_pk_bf8_f32(a, b, (int)old, HIGH));
 }
 
-// stochastic code of a scaled value: k = floor(u) + [frac(u) * 65536 > r + 0.5] with u = |t| in steps of the code's last place
+// Stochastic codes.  With u = |v| / scale in steps of the code's last place, k = floor(u) + [frac(u) * 65536 > r + 0.5] for 16 bits r,
+// in whole numbers, from the magnitude's bits m.  c = 65535 - r.
+//   normal codes: SHIFT = 23 - MAN mantissa bits f go, and the condition is f >= (r << SHIFT - 16) + 2^(SHIFT - 17) + 1: adding 2^SHIFT
+//     less that, (c << SHIFT - 16) + 2^(SHIFT - 17) - 1, carries into what stays, up to the exponent.  `add` holds the constant and
+//     takes the scale and the exponents' biases off.
+//   below them (steps of one size): the condition is ceil(u * 2^17) + 2 c reaching over into bit 17; the power of two is exact, so that
+//     nothing is rounded but by the ceil.
+// m is a normal number wherever its code is: with scales under -EMIN it need not be, and the values are scaled first (`fp8_drawn`).
+// Both shifts are made one, behind the choice.  Every value goes the one way: a way for normal codes alone, with this one where a patch
+// holds others, is 7 % faster where none does (27.3 us for 29.5 at 3001 x 5003) and 35 % slower where some do (46.6 for 34.5 at 4096 x 4096,
+// e4m3 from fp32).
 template <int FMT>
-__device__ __forceinline__ uint32_t fp8_stochastic(float t, uint32_t r16)
-{
+struct Fp8Draw {
     typedef Fp8Format<FMT> F;
-    const uint32_t b = __float_as_uint(t), m = b & 0x7FFFFFFFu, sign = (b >> 24) & 0x80u;
-    const uint32_t field = max(m >> 23, (uint32_t)(F::EMIN + 127));
-    const float u = __uint_as_float(m) * __uint_as_float((254u + F::MAN - field) << 23);
-    const float f = __builtin_floorf(u);
-    const uint32_t k = (uint32_t)(int)f + ((u - f) * 65536.0f > (float)r16 + 0.5f ? 1u : 0u);
-    const uint32_t code = ((field - (uint32_t)(F::EMIN + 127)) << F::MAN) + k;
-    const uint32_t special = FMT == Q8T_E4M3 ? 0x7Fu : (m > 0x7F800000u ? 0x7Fu : 0x7Cu);
-    return sign | (m >= 0x7F800000u ? special : code);
+    static constexpr int SHIFT = 23 - F::MAN;
+    int add, up;
+    uint32_t least;   // the smallest magnitude with a normal code (scale >= -EMIN)
+    __device__ __forceinline__ explicit Fp8Draw(uint32_t scale)   // stored
+    {
+        const int e = (int)scale - 127;
+        add = (1 << (SHIFT - 17)) - 1 - (int)((uint32_t)(e + 126 + F::EMIN) << 23);
+        up = 17 + F::MAN - F::EMIN - e;
+        least = (uint32_t)((int)scale + F::EMIN) << 23;
+    }
+    // the complement of the 16 bits where they are added
+    static __device__ __forceinline__ uint32_t drawn(uint32_t c16) { return c16 << (SHIFT - 16); }
+    __device__ __forceinline__ uint32_t code(uint32_t m, uint32_t drawn) const
+    {
+        const uint32_t steps = (uint32_t)__builtin_ceilf(__builtin_ldexpf(__uint_as_float(m), up));
+        return (m >= least ? m + drawn + (uint32_t)add : (steps << (SHIFT - 17)) + drawn) >> SHIFT;
+    }
+};
+
+// The code of any value v under any scale, given its inverse: scaled first, which is exact where the code is not 0.
+template <int FMT>
+__device__ __forceinline__ uint32_t fp8_drawn(float v, float inverse, uint32_t r16)
+{
+    const uint32_t b = __float_as_uint(v * inverse), m = b & 0x7FFFFFFFu, sign = b >> 24 & 0x80u;
+    const uint32_t special = FMT == Q8T_E4M3 || m > 0x7F800000u ? 0x7Fu : 0x7Cu;
+    return sign | (m >= 0x7F800000u ? special : Fp8Draw<FMT>(127u).code(m, Fp8Draw<FMT>::drawn(65535u - r16)));
 }
 
 // 8 codes of values v under the stored scale
@@ -70,7 +97,7 @@ __device__ __forceinline__ uint2 fp8_codes8(const float v[8], uint32_t scale, co
         } else {
             w[h] = 0u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[h] |= fp8_stochastic<FMT>(p[i] * inv, q8t_draw(r, 4 * h + i)) << (8 * i);
+            for (int i = 0; i < 4; ++i) w[h] |= fp8_drawn<FMT>(p[i], inv, q8t_draw(r, 4 * h + i)) << (8 * i);
         }
     }
     return make_uint2(w[0], w[1]);
@@ -83,10 +110,16 @@ __device__ __forceinline__ uint32_t fp8_max8(const float v[8])
     for (int i = 0; i < 8; ++i) m = max(m, fp8_magnitude(v[i]));
     return m;
 }
-// over 16 consecutive lanes (one block of 128 at eight entries a lane)
+// op over 16 consecutive lanes (one block of 128 at eight entries a lane); every one has the result
+template <class Op>
+__device__ __forceinline__ uint32_t fp8_fold16(uint32_t m, Op op)
+{
+    m = op(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, true));    // lanes 1 apart
+    m = op(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, true));    // 2 apart
+    m = op(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xF, 0xF, true));   // the other four of eight
+    return op(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x140, 0xF, 0xF, true));   // the other eight
+}
 __device__ __forceinline__ uint32_t fp8_max16(uint32_t m)
 {
-#pragma unroll
-    for (int off = 8; off > 0; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off, 64));
-    return m;
+    return fp8_fold16(m, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
