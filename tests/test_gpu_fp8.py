@@ -73,6 +73,24 @@ def test_special_values(fmt, stochastic):
     _check(x, q8t.fp8_quantize(x, fmt, stochastic=stochastic, seed=1, square=True, transposed=True), fmt, True, r)
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_scales_at_the_lower_end(fmt, dtype):
+    # blocks of a scale under the smallest normal number's, over rows, over columns, and next to others; denormal values among them
+    q8t = require_gpu()
+    import torch
+    g = np.random.default_rng(8)
+    x = g.standard_normal((260, 300)) * np.exp2(g.integers(-149, -90, (260, 300)))
+    x[:128, 128:] *= 2.0 ** 80
+    x[:, 7] *= 2.0 ** 30
+    x = torch.from_numpy(x).to(getattr(torch, dtype)).to("cuda:0")
+    r = plain.draws(260 * 300, 1)
+    for square in (False, True):
+        for both in (False, True):
+            _check(x, q8t.fp8_quantize(x, fmt, square=square, transposed=both), fmt, square, None)
+            _check(x, q8t.fp8_quantize(x, fmt, square=square, stochastic=True, seed=1, transposed=both), fmt, square, r)
+
+
 @pytest.mark.parametrize("dtype,off", [("float32", 1), ("bfloat16", 1), ("bfloat16", 3)])
 def test_quantize_view_at_an_offset(dtype, off):
     q8t = require_gpu()
@@ -178,6 +196,20 @@ def test_product_of_ordinary_values(M, N, K):
     plain.within(q8t.fp8_gemm(a, sa, b, sb, dtype=torch.float32), want, off, (M, N, K))
     off = off + 2.0 ** -10 * size
     plain.within(q8t.fp8_gemm(a, sa, b, sb), want, off + 2.0 ** -8 * (np.abs(want) + off), (M, N, K))
+
+
+@pytest.mark.parametrize("M,N,K", [(4101, 4093, 1100), (1024, 4090, 1500), (500, 4100, 3000), (1003, 3000, 2000), (8192, 260, 1000), (6000, 6100, 250),
+                                   (100, 9000, 5000), (1, 30000, 2000), (16, 20000, 1030)])
+def test_large_products(M, N, K):
+    # whole numbers whose sums stay below 2^24: the same in fp32 in any order
+    q8t = require_gpu()
+    import torch
+    a, sa, va = _operand(M, K, "e4m3", 5, whole=True)
+    b, sb, vb = _operand(N, K, "e5m2", 6, whole=True)
+    assert 144 * K < 2 ** 24
+    want = torch.from_numpy(va.astype(np.float32) @ vb.astype(np.float32).T)
+    assert torch.equal(q8t.fp8_gemm(a, sa, b, sb, torch.float32).cpu(), want)
+    assert torch.equal(q8t.fp8_gemm(a, sa, b, sb).cpu(), want.bfloat16())
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 100, 300), (40, 70, 260), (300, 300, 700), (520, 530, 256)])

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import lm_layer
 import lm_plain as plain
 import oracle
 
@@ -56,3 +57,18 @@ def test_gradients_against_differences():
         ins = [[v + (sign * 1e-5 * d if i == k else 0) for i, v in enumerate((res, h, gate, wp, wq))] for sign in (1, -1)]
         diff = (loss(*ins[0]) - loss(*ins[1])) / 2e-5
         assert abs(diff - (grads[k] * d).sum()) < 1e-7 * max(1, abs(diff))   # 1e-10 of the step, 1e-11 of the sums' rounding / 1e-5
+
+
+def test_gradients_of_a_block_against_differences():
+    x = lm_layer.inputs(6, 10, 7, 3)
+    out, grads = lm_layer.block(lm_layer.Exact(), x)
+
+    def loss(x):
+        out, _ = lm_layer.block(lm_layer.Exact(), x)
+        return (out["y2"] * x["dy"]).sum() + (out["res2"] * x["dres"]).sum()
+
+    g = np.random.default_rng(2)
+    for name, grad in grads.items():
+        d = g.standard_normal(grad.shape)
+        diff = (loss({**x, name: x[name] + 1e-5 * d}) - loss({**x, name: x[name] - 1e-5 * d})) / 2e-5
+        assert abs(diff - (grad * d).sum()) < 1e-6 * max(1, abs(diff)), name   # 1e-10 of the step, 1e-11 of the sums' rounding / 1e-5
