@@ -31,7 +31,7 @@ def _calls_commands():
            os.path.join(root, "include", "torch", "csrc", "api", "include"), "/opt/rocm/include"]
     compile_ = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
                 "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)] + ["-I" + i for i in inc]
-    link = ["g++", "-shared", "-o", CALLS, obj, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch", "-lc10", "-lc10_hip",
+    link = ["g++", "-shared", "-o", CALLS, obj, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch", "-ltorch_hip", "-lc10", "-lc10_hip",
             "-L" + HERE, "-l:libq8t.so", "-Wl,-rpath,$ORIGIN"]
     return compile_ + ["-c", os.path.join(CSRC, "python_calls.cpp"), "-o", obj], link
 

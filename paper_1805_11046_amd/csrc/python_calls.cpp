@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
@@ -149,17 +150,14 @@ struct Plane {   // N, C, H, W of a tensor
 };
 
 // ---- outputs and scratch memory ----
+// (past torch's dispatcher: 0.3 us less for each tensor, 4.9 us for 5.4 for a call with two)
 at::Tensor make(at::IntArrayRef shape, at::ScalarType type, const at::Tensor &like)
 {
     const Unlocked u;
-    return at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
+    return at::Tensor(at::detail::empty_cuda(shape, type, like.device(), std::nullopt));
 }
 at::Tensor make_params(const at::Tensor &like) { return make({6}, at::kInt, like); }
-at::Tensor same(const at::Tensor &like)
-{
-    const Unlocked u;
-    return at::empty_like(like);
-}
+at::Tensor same(const at::Tensor &like) { return make(like.sizes(), like.scalar_type(), like); }   // like is contiguous
 // the tensor handed in, or a new one
 template <class F>
 at::Tensor given(PyObject *o, F fresh)
@@ -697,7 +695,8 @@ PyObject *residual_norm_fwd(Argv a)
     const double p = wide(a[8]);
     const uint64_t s0 = seed(a[9]);
     const int64_t *step = counter(a[10], res);
-    const bool pre = w_pre.defined(), quantized = pre && truth(a[11]);
+    const bool pre = w_pre.defined(), quantized = truth(a[11]);
+    if (quantized && !pre) raise(PyExc_ValueError, "q8t: the codes are those of y, which needs w_pre");
     at::Tensor res_out, y, q, s;
     if (h.defined()) res_out = same(res);
     if (pre && (truth(a[12]) || !quantized)) y = same(res);

@@ -295,7 +295,7 @@ def test_refusals():
     for k in (dict(h=x["h"][:3]), dict(h=x["h"].bfloat16()), dict(w_post=x["w_post"][:32]), dict(w_post=x["w_post"].bfloat16()), dict(gate=x["gate"][0]),
               dict(gate=x["gate"][:, :32].contiguous()), dict(gate=torch.ones(4, 64, device="cuda:0")), dict(w_pre=x["w_pre"].double()), dict(h=None),
               dict(p=-1.0), dict(p=2.0), dict(h=None, w_post=None, gate=None, p=0.5), dict(h=None, w_post=None, gate=None, res_scale=2.0),
-              dict(h=None, w_post=None, gate=None, w_pre=None), dict(h=x["h"].t().contiguous().t()), dict(w_pre=x["w_pre"].cpu())):
+              dict(h=None, w_post=None, gate=None, w_pre=None), dict(w_pre=None, quantized=True), dict(h=x["h"].t().contiguous().t()), dict(w_pre=x["w_pre"].cpu())):
         with pytest.raises((ValueError, q8t.Q8TError)):
             f(**k)
     with pytest.raises(q8t.Q8TError, match="SHAPE"):
