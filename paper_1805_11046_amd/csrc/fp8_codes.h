@@ -41,48 +41,45 @@ __device__ __forceinline__ uint32_t fp8_pack2(float a, float b, uint32_t old)
 }
 
 // Stochastic codes.  With u = |v| / scale in steps of the code's last place, k = floor(u) + [frac(u) * 65536 > r + 0.5] for 16 bits r,
-// in whole numbers, from the magnitude's bits m.  c = 65535 - r.
-//   normal codes: SHIFT = 23 - MAN mantissa bits f go, and the condition is f >= (r << SHIFT - 16) + 2^(SHIFT - 17) + 1: adding 2^SHIFT
-//     less that, (c << SHIFT - 16) + 2^(SHIFT - 17) - 1, carries into what stays, up to the exponent.  `add` holds the constant and
-//     takes the scale and the exponents' biases off.
-//   below them (steps of one size): the condition is ceil(u * 2^17) + 2 c reaching over into bit 17; the power of two is exact, so that
-//     nothing is rounded but by the ceil.
-// m is a normal number wherever its code is: with scales under -EMIN it need not be, and the values are scaled first (`fp8_drawn`).
-// Both shifts are made one, behind the choice.  Every value goes the one way: a way for normal codes alone, with this one where a patch
-// holds others, is 7 % faster where none does (27.3 us for 29.5 at 3001 x 5003) and 35 % slower where some do (46.6 for 34.5 at 4096 x 4096,
-// e4m3 from fp32).
+// in whole numbers.  c = 65535 - r.
+//   normal codes: of the magnitude's bits m, SHIFT = 23 - MAN mantissa bits f go, and the condition is f >= (r << SHIFT - 16) +
+//     2^(SHIFT - 17) + 1: adding 2^SHIFT less that, (c << SHIFT - 16) + 2^(SHIFT - 17) - 1, carries into what stays, up to the exponent.
+//   below them all steps are of one size: |v| + least, `least` the smallest magnitude with a normal code, has the mantissa that the sum
+//     above wants and an exponent one too high.  That sum has to be rounded up, so that a fraction just over the border stays over it.
+// The larger of m and the second is the right one on both sides of `least`.  Needs fp8_round_up, and least >= 2^-126, that is scales
+// above -EMIN; under others the values are scaled first (fp8_drawn), which is exact where the code is not 0.
 template <int FMT>
 struct Fp8Draw {
     typedef Fp8Format<FMT> F;
     static constexpr int SHIFT = 23 - F::MAN;
-    int add, up;
-    uint32_t least;   // the smallest magnitude with a normal code (scale >= -EMIN)
-    __device__ __forceinline__ explicit Fp8Draw(uint32_t scale)   // stored
-    {
-        const int e = (int)scale - 127;
-        add = (1 << (SHIFT - 17)) - 1 - (int)((uint32_t)(e + 126 + F::EMIN) << 23);
-        up = 17 + F::MAN - F::EMIN - e;
-        least = (uint32_t)((int)scale + F::EMIN) << 23;
-    }
-    // the complement of the 16 bits where they are added
-    static __device__ __forceinline__ uint32_t drawn(uint32_t c16) { return c16 << (SHIFT - 16); }
+    uint32_t least;
+    __device__ __forceinline__ explicit Fp8Draw(uint32_t scale) : least((uint32_t)((int)scale + F::EMIN) << 23) {}   // stored scale
+    // 16 bits where they are added
+    static __device__ __forceinline__ uint32_t drawn(uint32_t r16) { return ((65535u - r16) << (SHIFT - 16)) + (1u << (SHIFT - 17)) - 1u; }
     __device__ __forceinline__ uint32_t code(uint32_t m, uint32_t drawn) const
     {
-        const uint32_t steps = (uint32_t)__builtin_ceilf(__builtin_ldexpf(__uint_as_float(m), up));
-        return (m >= least ? m + drawn + (uint32_t)add : (steps << (SHIFT - 17)) + drawn) >> SHIFT;
+        const uint32_t low = __float_as_uint(__uint_as_float(m) + __uint_as_float(least));
+        return (max(m + 0x800000u, low) + drawn - least) >> SHIFT;
     }
 };
-
-// The code of any value v under any scale, given its inverse: scaled first, which is exact where the code is not 0.
+// From here on additions in fp32 are rounded up in this wavefront, those of anything that is computed from the words given among them.
+template <int N>
+__device__ __forceinline__ void fp8_round_up(uint32_t (&first)[N])
+{
+    asm volatile("s_setreg_imm32_b32 hwreg(HW_REG_MODE, 0, 2), 1\n\ts_nop 3" : "+v"(first[0]));
+#pragma unroll
+    for (int i = 1; i < N; ++i) asm volatile("" : "+v"(first[i]));
+}
+// The code of any value v under any scale, given its inverse.
 template <int FMT>
-__device__ __forceinline__ uint32_t fp8_drawn(float v, float inverse, uint32_t r16)
+__device__ __forceinline__ uint32_t fp8_drawn(float v, float inverse, uint32_t drawn)
 {
     const uint32_t b = __float_as_uint(v * inverse), m = b & 0x7FFFFFFFu, sign = b >> 24 & 0x80u;
     const uint32_t special = FMT == Q8T_E4M3 || m > 0x7F800000u ? 0x7Fu : 0x7Cu;
-    return sign | (m >= 0x7F800000u ? special : Fp8Draw<FMT>(127u).code(m, Fp8Draw<FMT>::drawn(65535u - r16)));
+    return sign | (m >= 0x7F800000u ? special : Fp8Draw<FMT>(127u).code(m, drawn));
 }
 
-// 8 codes of values v under the stored scale
+// 8 codes of values v under the stored scale (STOCH: behind fp8_round_up)
 template <int FMT, bool STOCH>
 __device__ __forceinline__ uint2 fp8_codes8(const float v[8], uint32_t scale, const uint32_t r[4])
 {
@@ -97,7 +94,7 @@ __device__ __forceinline__ uint2 fp8_codes8(const float v[8], uint32_t scale, co
         } else {
             w[h] = 0u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[h] |= fp8_drawn<FMT>(p[i], inv, q8t_draw(r, 4 * h + i)) << (8 * i);
+            for (int i = 0; i < 4; ++i) w[h] |= fp8_drawn<FMT>(p[i], inv, Fp8Draw<FMT>::drawn(q8t_draw(r, 4 * h + i))) << (8 * i);
         }
     }
     return make_uint2(w[0], w[1]);
