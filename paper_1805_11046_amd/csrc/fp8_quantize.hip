@@ -115,10 +115,10 @@ __device__ __forceinline__ uint2 any8(const Q8tEight<T> &x, const uint32_t drawn
 
 // Both copies of a 128 x 128 tile from one read; every thread holds a patch of 8 x 8, so that it packs eight codes along
 // either axis.  SQUARE: one scale for the tile, and the transposed copy holds the same codes.
-// Bound by memory where the rounding is to nearest: both copies of 8192 x 8192 from bf16 in 53.5 us, the time of a copy of as many bytes;
-// one scale a tile of 4096 x 4096 from fp32 in 24.7 for 20.  Stochastic by the vector instructions, half of them the generator's, in
-// three groups of four for eight entries where a row starts inside a group: 3001 x 5003 from bf16 in 26.9 us, 3008 x 5008 in 24.5, for 12;
-// all tiles are on the card at once there and read, compute and write together.  8192 x 8192 takes 69.7.
+// Bound by memory where the rounding is to nearest: both copies of 8192 x 8192 from bf16 in 51.5 us, the time of a copy of as many bytes;
+// one scale a tile of 4096 x 4096 from fp32 in 24.3 for 20.  Stochastic by the vector instructions, half of them the generator's, in
+// three groups of four for eight entries where a row starts inside a group: 3001 x 5003 from bf16 in 26.4 us, 3008 x 5008 in 23.2, for 12;
+// all tiles are on the card at once there and read, compute and write together.  8192 x 8192 takes 68.1.
 template <class T, int FMT, bool STOCH, bool ALIGNED, bool SQUARE>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void quantize_tile(const T *__restrict__ x, int64_t R, int64_t C, uint32_t nbr, uint32_t nbc,
                                                           uint64_t seed, const int64_t *__restrict__ step, uint8_t *__restrict__ q,
@@ -127,7 +127,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void quantize_til
     typedef Magnitudes<T> Mag;
     constexpr int N = Mag::N;
     __shared__ uint32_t colmax[4][16][N];
-    __shared__ __align__(16) uint8_t turned[128][144];
+    // the codes by columns, 16 bytes of rows in a piece; a patch's columns have their pieces in an order of their own, and columns from 64 on
+    // lie half of the banks further, so that the lanes of a store have banks of their own; rows of 144 bytes: 27.1 us for 24.3 at 4096 x 4096 from fp32
+    __shared__ __align__(16) uint8_t turned[129 * 128];
+    auto place = [](int col, int piece) { return col * 128 + (col >> 6) * 128 + ((piece ^ (col >> 3 & 7)) << 4); };
     const uint32_t tr = blockIdx.x / nbc, tc = blockIdx.x - tr * nbc;
     const int ty = threadIdx.x / 16, tx = threadIdx.x & 15, wave = threadIdx.x / 64;
     const int64_t r0 = (int64_t)tr * 128 + ty * 8, c0 = (int64_t)tc * 128 + tx * 8;
@@ -262,7 +265,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void quantize_til
         turn4(half(0), half(1), half(2), half(3), up);
         turn4(half(4), half(5), half(6), half(7), down);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) *reinterpret_cast<uint2 *>(&turned[tx * 8 + 4 * h + j][ty * 8]) = make_uint2(up[j], down[j]);
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<uint2 *>(&turned[place(tx * 8 + 4 * h + j, ty >> 1) + (ty & 1) * 8]) = make_uint2(up[j], down[j]);
     }
     if (ty == 0) {
 #pragma unroll
@@ -277,9 +280,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void quantize_til
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const int piece = k * kThreads + threadIdx.x, col = piece / 8, at = (piece & 7) * 16;
+        const int piece = k * kThreads + threadIdx.x, col = piece / 8, part = piece & 7;
         const int64_t c = (int64_t)tc * 128 + col;
-        if (c < C) *reinterpret_cast<uint4 *>(qt + c * nbr * 128 + (int64_t)tr * 128 + at) = *reinterpret_cast<const uint4 *>(&turned[col][at]);
+        if (c < C) *reinterpret_cast<uint4 *>(qt + c * nbr * 128 + (int64_t)tr * 128 + part * 16) = *reinterpret_cast<const uint4 *>(&turned[place(col, part)]);
     }
 }
 
