@@ -609,6 +609,11 @@ const int64_t *counter(PyObject *o, const at::Tensor &first)
     if (t.scalar_type() != at::kLong || t.numel() != 1) raise(PyExc_ValueError, "q8t: step is a tensor of one int64");
     return ptr<int64_t>(t);
 }
+// scratch memory that is handed in
+void holds(PyObject *ws, size_t need, const at::Tensor &first)
+{
+    if (ws != Py_None && beside(ws, first).nbytes() < need) raise(PyExc_ValueError, "q8t: ws is smaller than the call needs");
+}
 int64_t code_bytes(int64_t n) { return (n + 127) / 128 * 128; }
 int64_t scale_bytes(int64_t n) { return (n + 511) / 512 * 4; }
 
@@ -627,6 +632,7 @@ PyObject *fp8_quantize(Argv a)
     const at::Tensor q = result(a[7], x, {R, code_bytes(C)}, code, what);
     const at::Tensor s = result(a[8], x, {R, scale_bytes(C)}, at::kFloat8_e8m0fnu, what);
     at::Tensor qt, st;
+    if (!truth(a[6]) && (a[9] != Py_None || a[10] != Py_None)) raise(PyExc_ValueError, "q8t: qt_out and st_out go with transposed=True");
     if (truth(a[6])) {
         qt = result(a[9], x, {C, code_bytes(R)}, code, what);
         st = result(a[10], x, {C, scale_bytes(R)}, at::kFloat8_e8m0fnu, what);
@@ -653,7 +659,9 @@ PyObject *fp8_gemm(Argv v)
     is(sb, {b.size(0), scale_bytes(K)}, at::kFloat8_e8m0fnu, what);
     const int M = Plane::dim(a.size(0)), N = Plane::dim(b.size(0)), k = Plane::dim(K);
     const at::Tensor out = result(v[5], a, {M, N}, type == Q8T_F32 ? at::kFloat : at::kBFloat16, "q8t: out has another shape or type than the result");
-    const Scratch ws(v[6], q8t_fp8_gemm_workspace_size(M, N, k), v[0], true);
+    const size_t need = q8t_fp8_gemm_workspace_size(M, N, k);
+    holds(v[6], need, a);
+    const Scratch ws(v[6], need, v[0], true);
     run("q8t_fp8_gemm", [&, w = ws.get()](void *stream) {
         return q8t_fp8_gemm(ptr<uint8_t>(a), ptr<uint8_t>(sa), fa, ptr<uint8_t>(b), ptr<uint8_t>(sb), fb, M, N, k, ptr<void>(out), type, w, stream);
     });
@@ -739,7 +747,9 @@ PyObject *residual_norm_bwd(Argv a)
     if (gate.defined()) dgate = same(gate);
     if (w_post.defined()) dw_post = make({n.D}, at::kFloat, r);
     if (w_pre.defined()) dw_pre = make({n.D}, at::kFloat, r);
-    const Scratch ws(a[13], q8t_residual_norm_bwd_workspace_size(n.T, n.D, groups), a[2]);
+    const size_t need = q8t_residual_norm_bwd_workspace_size(n.T, n.D, groups);
+    holds(a[13], need, r);
+    const Scratch ws(a[13], need, a[2]);
     run("q8t_residual_norm_bwd", [&, w = ws.get()](void *stream) {
         return q8t_residual_norm_bwd(ptr<void>(dy), ptr<void>(dres_out), ptr<void>(r), ptr<void>(h), ptr<float>(stats), ptr<float>(w_post),
                                      ptr<void>(gate), groups, ptr<float>(w_pre), type, n.T, n.D, res_scale, branch_scale, p, s0, step,

@@ -228,6 +228,25 @@ def test_a_nan_stays_in_its_row(M, N, K):
     assert np.array_equal(got[clean], (va @ vb.T)[clean])
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 100, 300), (40, 70, 260), (300, 300, 700), (520, 530, 256), (600, 3000, 256)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_a_scale_that_is_none_stays_in_its_row(M, N, K, dtype):
+    # scale 255 stands for NaN
+    q8t = require_gpu()
+    import torch
+    a, sa, va = _operand(M, K, "e4m3", 1, whole=True)
+    b, sb, vb = _operand(N, K, "e5m2", 2, whole=True)
+    m, n = M - 1, N // 2
+    sa.view(torch.uint8)[m, 1] = 255
+    sb.view(torch.uint8)[n, 0] = 255
+    got = q8t.fp8_gemm(a, sa, b, sb, dtype=getattr(torch, dtype))
+    clean = np.ones((M, N), bool)
+    clean[m, :] = clean[:, n] = False
+    assert np.isnan(plain.host(got)[~clean]).all()
+    want = torch.from_numpy(va @ vb.T).to(torch.float32).to(got.dtype)
+    assert np.array_equal(plain.host(got)[clean], plain.host(want)[clean])
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 130, 300), (37, 100, 200), (260, 300, 300), (513, 514, 1280)])
 def test_product_writes_its_rows_alone(M, N, K):
     q8t = require_gpu()
@@ -337,9 +356,15 @@ def test_refusals():
                  lambda: q8t.fp8_gemm(q, s, q[:, :128].contiguous(), s), lambda: q8t.fp8_gemm(q, s[:4], q, s),
                  lambda: q8t.fp8_gemm(q.view(torch.uint8), s, q, s), lambda: q8t.fp8_gemm(q, s.view(torch.uint8), q, s),
                  lambda: q8t.fp8_gemm(q, s, q, s, out=torch.zeros(8, 8, device="cuda:0")), lambda: q8t.fp8_gemm(q, s, q.cpu(), s),
+                 lambda: q8t.fp8_quantize(x, qt_out=torch.empty(256, 128, dtype=torch.float8_e4m3fn, device="cuda:0")),
+                 lambda: q8t.fp8_gemm(q, s, q, s, ws=torch.empty(16, device="cuda:0").t()[:0].cpu()),
                  lambda: q8t.fp8_gemm(q[:, 64:192], s, q, s), lambda: q8t.fp8_gemm(q[:, :0], s[:, :0], q[:, :0], s[:, :0])):
         with pytest.raises((ValueError, q8t.Q8TError)):
             call()
+    a, sa, _, _ = q8t.fp8_quantize(torch.zeros(512, 8192, device="cuda:0"))     # summed in slices
+    assert q8t.binding._lib.q8t_fp8_gemm_workspace_size(512, 512, 8192) > 1024
+    with pytest.raises(ValueError, match="ws"):
+        q8t.fp8_gemm(a, sa, a, sa, ws=torch.empty(1024, dtype=torch.uint8, device="cuda:0"))
     flat = torch.zeros(8 * 256 + 8, dtype=torch.uint8, device="cuda:0")
     odd = flat[8:].view(8, 256).view(torch.float8_e4m3fn)        # 8 bytes off a 16-byte address
     for call in (lambda: q8t.fp8_gemm(odd, s, q, s), lambda: q8t.fp8_gemm(q, s, odd, s), lambda: q8t.fp8_quantize(x, q_out=odd)):

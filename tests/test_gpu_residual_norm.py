@@ -305,6 +305,7 @@ def test_refusals():
     b = lambda *a, **k: q8t.residual_norm_bwd(*a, **{**dict(w_post=x["w_post"], gate=x["gate"], w_pre=x["w_pre"]), **k})   # noqa: E731
     for a, k in (((None, None, out[0], x["h"], out[2]), {}), ((x["dy"], None, out[0], None, out[2]), {}), ((x["dy"], None, out[0], x["h"], None), {}),
                  ((x["dy"], None, out[0], x["h"], out[2][:, :3].contiguous()), {}), ((x["dy"], None, out[0], x["h"], out[2]), dict(w_pre=None)),
-                 ((x["dy"].bfloat16(), None, out[0], x["h"], out[2]), {})):
+                 ((x["dy"].bfloat16(), None, out[0], x["h"], out[2]), {}),
+                 ((x["dy"], None, out[0], x["h"], out[2]), dict(ws=torch.empty(16, device="cuda:0")))):
         with pytest.raises((ValueError, q8t.Q8TError)):
             b(*a, **k)
