@@ -637,7 +637,7 @@ def fp8_quantize(x, fmt="e4m3", square=False, stochastic=False, seed=0, step=Non
     """Codes of a matrix [R, C] in 8-bit floating point ("e4m3", "e5m2") with a power of two as scale of every 128 entries of a row,
     or of every 128 x 128 block (square).  Returns (q, s, qt, st): q [R, C filled up to 128] codes and s [R, one a block, filled up to a
     multiple of 4] scales (float8_e8m0fnu); with transposed=True the copy whose blocks run down the columns as well, qt [C, R filled
-    up to 128] and st, else None."""
+    up to 128] and st, else None (and qt_out, st_out as they were)."""
     return _calls.fp8_quantize(x, _one_of(_FORMATS, fmt, "fmt"), square, stochastic, seed, step, transposed, q_out, s_out, qt_out, st_out)
 
 

@@ -14,8 +14,7 @@ int q8t_fp8_product_f32(const Fp8Product &p, int fa, int fb, const Fp8Plan &plan
             return rc || plan.slices == 1 ? rc : run_fold<float>(p, plan.slices, ws, st);
         }
         case FP8_TILE_64_128: return run_tiles<A, B, true, float, Tile<64, 128, 32, 64, 2>>(p, 1, ws, st);
-        case FP8_TILE_128:
-        case FP8_TILE_128_DEEP: return run_tiles<A, B, true, float, Tile<128, 128, 64, 64, 2>>(p, 1, ws, st);
+        case FP8_TILE_128: return run_tiles<A, B, true, float, Tile<128, 128, 64, 64, 2>>(p, 1, ws, st);
         default: return run_tiles<A, B, true, float, Tile<256, 256, 128, 64, 2>>(p, 1, ws, st);
         }
     });

@@ -632,7 +632,6 @@ PyObject *fp8_quantize(Argv a)
     const at::Tensor q = result(a[7], x, {R, code_bytes(C)}, code, what);
     const at::Tensor s = result(a[8], x, {R, scale_bytes(C)}, at::kFloat8_e8m0fnu, what);
     at::Tensor qt, st;
-    if (!truth(a[6]) && (a[9] != Py_None || a[10] != Py_None)) raise(PyExc_ValueError, "q8t: qt_out and st_out go with transposed=True");
     if (truth(a[6])) {
         qt = result(a[9], x, {C, code_bytes(R)}, code, what);
         st = result(a[10], x, {C, scale_bytes(R)}, at::kFloat8_e8m0fnu, what);

@@ -98,6 +98,7 @@ struct NormWaves {
 };
 
 // Rows one after the other, a row's inputs asked for while the one before it is still worked on; the weights stay in registers.
+// 8192 x 4096 bf16 with everything: 53 us, 5.1 TB/s, the rate of a copy; 6000 x 5120 53.5.
 template <class T, class S, bool H, bool POST, bool GATE, bool DROP>
 __global__ __launch_bounds__(S::WAVE ? 256 : S::MOST, (NormWaves<T, S>::FWD)) void norm_fwd(const Norm a)
 {
@@ -280,8 +281,8 @@ constexpr int norm_bwd_lds()   // bytes a thread
 enum { GATE_NONE, GATE_SHARED, GATE_ROWS };   // a row of the gate for several rows, for each
 // What a call of the backward pass has.  Known when compiled: both gradients, the norm in front and a block output, rows of a multiple of
 // eight entries.  Then no load or store hangs on a condition, threads behind the row's end do the last eight entries' work along with
-// their owner, and the compiler can count what is under way: a wait for one row's tensors does not become one for the next row's, which
-// have just been asked for.  Both passes over the rows and the sums, 6000 x 5120 bf16, us: conditional 125, known 103.
+// their owner (which is in the same wavefront, so that dres may lie where dy or dres_out does), and the compiler can count what is
+// under way: a wait for one row's tensors does not become one for the next row's, which have just been asked for.  Both passes over the rows and the sums, 6000 x 5120 bf16, us: conditional 125, known 94.
 template <bool POST, int GATE, bool DROP>
 struct BackKnown {
     static constexpr bool h = true, pre = true, out = true, post = POST, drop = DROP, even = true;
@@ -299,7 +300,8 @@ struct BackAsked {
 };
 
 // One workgroup a chunk of rows: the column sums go to the workspace once; the tensors of the next row are asked for as soon as this
-// row's have been used, into the same registers.
+// row's have been used, into the same registers.  6000 x 5120 bf16 with a shared gate and drop-out: 87 us, 4.8 TB/s with the 31 MB of
+// partial sums that 500 workgroups leave; fewer would not hide their loads.
 template <class T, class S, class F>
 __global__ __launch_bounds__(S::MOST, (NormWaves<T, S>::BWD)) void norm_bwd(const NormBack a)
 {
