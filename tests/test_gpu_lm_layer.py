@@ -177,3 +177,25 @@ def test_tokens_to_answers(T, dtype):
         eager = step(x["res"] * sign)
         torch.cuda.synchronize()
         assert all((a is None and b is None) or torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(again, eager))
+
+
+def test_outputs_are_ordinary_tensors():
+    # in and out of inference mode, with the storage of a tensor that torch makes
+    q8t = require_gpu()
+    import torch
+    x = _inputs(6, 256, 64, 1, torch.bfloat16)
+
+    def outputs():
+        return [t for t in q8t.residual_norm_fwd(x["res"], x["res"], w_pre=x["w_pre"], quantized=True) if t is not None] + \
+            [t for t in q8t.fp8_quantize(x["w1"], transposed=True)] + [q8t.dropout(x["res"], 0.5)]
+
+    for t in outputs():
+        assert not t.is_inference() and t.is_contiguous() and t.storage_offset() == 0 and t.untyped_storage().nbytes() >= t.numel() * t.element_size()
+    y = outputs()[1]
+    y.requires_grad_(True)
+    (y.float() * 2).sum().backward()
+    assert torch.equal(y.grad.float(), torch.full_like(y.float(), 2.0))
+    with torch.inference_mode():
+        assert all(t.is_inference() for t in outputs())
+        z = outputs()[-1].add_(1)
+    assert z.shape == x["res"].shape
