@@ -66,14 +66,21 @@ int q8t_norm_bwd_bf16(const NormBack &a, const NormCall &c, int64_t chunks, hipS
 
 namespace {
 
-// Sum over the threads of a row; every thread has it.  WAVE: a row is one wavefront's, else the workgroup's.  scratch: two sets of slots
-// used in turn, so that one barrier a sum does.
-template <bool WAVE>
+// MOST threads a row at most (up to 64: LANES of one wavefront, which has 64 / LANES rows at a time; else a workgroup), NV vectors of eight
+// entries a thread; TINY: rows of fewer than eight.  A row's 16 lanes are the fewest, as many as hold a block of codes.
+template <int MOST_, int NV_, bool TINY_>
+struct NormShape {
+    static constexpr int MOST = MOST_, NV = NV_, LANES = MOST < 64 ? MOST : 64, ROWS = 64 / LANES;
+    static constexpr bool WAVE = MOST <= 64, TINY = TINY_;
+};
+
+// Sum over the threads of a row; every thread has it.  scratch: two sets of slots used in turn, so that one barrier a sum does.
+template <class S>
 __device__ __forceinline__ float row_sum(float v, float (*scratch)[16], int &turn)
 {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    if (WAVE) return v;
+    for (int off = S::LANES / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    if (S::WAVE) return v;
     float *slot = scratch[turn];
     turn ^= 1;
     if ((threadIdx.x & 63) == 0) slot[threadIdx.x / 64] = v;
@@ -84,17 +91,11 @@ __device__ __forceinline__ float row_sum(float v, float (*scratch)[16], int &tur
     return t;
 }
 
-// MOST threads a row at most (64: one wavefront), NV vectors of eight entries a thread; TINY: rows of fewer than eight
-template <int MOST_, int NV_, bool TINY_>
-struct NormShape {
-    static constexpr int MOST = MOST_, NV = NV_;
-    static constexpr bool WAVE = MOST == 64, TINY = TINY_;
-};
 // wavefronts of a SIMD that the registers have to allow, so that enough loads are in flight
 template <class T, class S>
 struct NormWaves {
     static constexpr bool SHORT = sizeof(T) == 2;
-    static constexpr int FWD = S::NV == 1 && SHORT ? 6 : 4, BWD = S::WAVE ? (SHORT ? 4 : 3) : 4;
+    static constexpr int FWD = S::NV == 1 && SHORT && S::ROWS == 1 ? 6 : 4, BWD = S::WAVE ? (SHORT && S::ROWS == 1 ? 4 : 3) : 4;
 };
 
 // Rows one after the other, a row's inputs asked for while the one before it is still worked on; the weights stay in registers.
@@ -106,10 +107,11 @@ __global__ __launch_bounds__(S::WAVE ? 256 : S::MOST, (NormWaves<T, S>::FWD)) vo
     constexpr bool WAVE = S::WAVE, TINY = S::TINY;
     __shared__ float scratch[2][16];
     int turn = 0;
-    const uint32_t TH = WAVE ? 64 : blockDim.x, t = WAVE ? threadIdx.x & 63 : threadIdx.x, D = a.D;
-    const int64_t stride = WAVE ? (int64_t)gridDim.x * 4 : gridDim.x;
-    int64_t row = WAVE ? (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : blockIdx.x;
-    if (row >= a.T) return;   // a whole wavefront; a workgroup of several has a row
+    const uint32_t TH = WAVE ? 64 : blockDim.x, t = WAVE ? threadIdx.x & (S::LANES - 1) : threadIdx.x, D = a.D;
+    const int64_t stride = WAVE ? (int64_t)gridDim.x * 4 * S::ROWS : gridDim.x;
+    int64_t row = WAVE ? ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64)) * S::ROWS : blockIdx.x;
+    if (S::ROWS > 1) row += threadIdx.x % 64 / S::LANES;
+    if (row >= a.T) return;   // all threads of the row; a workgroup of several wavefronts has one
     const float rD = 1.0f / (float)D;
     const Q8tSeed sd = DROP ? q8t_seed(a.seed, a.step) : Q8tSeed{0, 0};
     const float scale = DROP ? a.branch_scale * a.d.scale : a.branch_scale;
@@ -146,7 +148,7 @@ __global__ __launch_bounds__(S::WAVE ? 256 : S::MOST, (NormWaves<T, S>::FWD)) vo
                     for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(xh[j][i], xh[j][i], ss);
 #pragma unroll
                 for (int j = 0; j < NV; ++j) xh[j].hold();
-                rstd = 1.0f / __builtin_sqrtf(row_sum<WAVE>(ss, scratch, turn) * rD + a.eps);
+                rstd = 1.0f / __builtin_sqrtf(row_sum<S>(ss, scratch, turn) * rD + a.eps);
             }
             if (a.stats && t == 0) a.stats[row] = rstd;
             const float factor = rstd * scale;   // all that is the same for the row
@@ -191,7 +193,7 @@ __global__ __launch_bounds__(S::WAVE ? 256 : S::MOST, (NormWaves<T, S>::FWD)) vo
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(r[j][i], r[j][i], ss);
-        const float rstd = 1.0f / __builtin_sqrtf(row_sum<WAVE>(ss, scratch, turn) * rD + a.eps);
+        const float rstd = 1.0f / __builtin_sqrtf(row_sum<S>(ss, scratch, turn) * rD + a.eps);
         if (a.stats && t == 0) a.stats[a.T + row] = rstd;
         const uint32_t nb = (D + 127) / 128, sp = (nb + 3) & ~3u;
 #pragma unroll
@@ -279,18 +281,20 @@ constexpr int norm_bwd_lds()   // bytes a thread
 }
 
 enum { GATE_NONE, GATE_SHARED, GATE_ROWS };   // a row of the gate for several rows, for each
-// What a call of the backward pass has.  Known when compiled: both gradients, the norm in front and a block output, rows of a multiple of
-// eight entries.  Then no load or store hangs on a condition, threads behind the row's end do the last eight entries' work along with
-// their owner (which is in the same wavefront, so that dres may lie where dy or dres_out does), and the compiler can count what is
-// under way: a wait for one row's tensors does not become one for the next row's, which have just been asked for.  Both passes over the rows and the sums, 6000 x 5120 bf16, us: conditional 125, known 94.
-template <bool POST, int GATE, bool DROP>
+// What a call of the backward pass has.  Known when compiled: both gradients, the norm in front and a block output, rows of eight entries at
+// least.  Then no load or store hangs on a condition, and the compiler can count what is under way: a wait for one row's tensors does not
+// become one for the next row's, which have just been asked for.  So every thread has eight whole entries: those behind the row's end do
+// the last eight's work along with their owner; where D is no multiple of eight, the second thread's begin among the first one's, and the
+// sums over the row leave out what is another's.  Such threads are in one wavefront, so that dres may lie where dy or dres_out does.
+// Both passes over the rows and the sums, 6000 x 5120 bf16, us: conditional 125, known 94.
+template <bool POST, int GATE, bool DROP, bool EVEN>
 struct BackKnown {
-    static constexpr bool h = true, pre = true, out = true, post = POST, drop = DROP, even = true;
+    static constexpr bool h = true, pre = true, out = true, post = POST, drop = DROP, known = true, even = EVEN;
     static constexpr int gate = GATE;
     __device__ explicit BackKnown(const NormBack &) {}
 };
 struct BackAsked {
-    static constexpr bool even = false;
+    static constexpr bool known = false, even = false;
     bool h, pre, out, post, drop;
     int gate;
     __device__ explicit BackAsked(const NormBack &a)
@@ -303,40 +307,58 @@ struct BackAsked {
 // row's have been used, into the same registers.  6000 x 5120 bf16 with a shared gate and drop-out: 87 us, 4.8 TB/s with the 31 MB of
 // partial sums that 500 workgroups leave; fewer would not hide their loads.
 template <class T, class S, class F>
-__global__ __launch_bounds__(S::MOST, (NormWaves<T, S>::BWD)) void norm_bwd(const NormBack a)
+__global__ __launch_bounds__(S::WAVE ? 64 : S::MOST, (NormWaves<T, S>::BWD)) void norm_bwd(const NormBack a)
 {
     constexpr int NV = S::NV;
-    constexpr bool WAVE = S::WAVE, TINY = S::TINY, EVEN = F::even, WEIGHTS_KEPT = NV == 1;
+    constexpr bool WAVE = S::WAVE, TINY = S::TINY, KNOWN = F::known, WEIGHTS_KEPT = NV == 1;
     extern __shared__ float4 kept[];
     __shared__ float scratch[2][16];
     int turn = 0;
     const F f(a);
-    const uint32_t t = threadIdx.x, D = a.D, TH = WAVE ? 64 : blockDim.x;
+    const uint32_t t = WAVE ? threadIdx.x & (S::LANES - 1) : threadIdx.x, D = a.D, TH = WAVE ? 64 : blockDim.x;
     const float rD = 1.0f / (float)D;
     int64_t first, last;
     rows_of_chunk(a, blockIdx.x, first, last);
+    if (S::ROWS > 1) {   // a part of the chunk for each row that the wavefront has at a time, of whole groups where the chunk is
+        const int64_t unit = f.gate == GATE_SHARED && !a.group_chunks ? a.group_rows : 1;
+        const int64_t rows = ((last - first) / unit + S::ROWS - 1) / S::ROWS * unit;
+        first = min(first + (int64_t)(threadIdx.x / S::LANES) * rows, last);
+        last = min(first + rows, last);
+    }
     const Q8tSeed sd = f.drop ? q8t_seed(a.seed, a.step) : Q8tSeed{0, 0};
     const float scale = f.drop ? a.branch_scale * a.d.scale : a.branch_scale;
-    const LdsEights lds = {kept + t, TH};
+    const LdsEights lds = {kept + threadIdx.x, TH};
     RowSums<S> sums;
     sums.lds = lds;
 #pragma unroll
     for (int k = 0; k < 3; ++k) sums.clear(k);
 
-    auto col = [&](int j) -> uint32_t {
-        const uint32_t c = (j * TH + t) * 8;
-        return EVEN ? min(c, D - 8) : c;
+    const uint32_t eights = (D + 7) / 8, shared = eights * 8 - D;
+    auto col = [&](int j) -> uint32_t {   // the first of a thread's eight entries
+        const uint32_t k = j * TH + t;
+        if (!KNOWN) return k * 8;
+        return min(!F::even && k ? k * 8 - shared : k * 8, D - 8);
     };
-    auto own = [&](int j) { return (j * TH + t) * 8 < D; };
+    auto others = [&](int j) -> int {   // how many of them, from the first on, are another thread's
+        const uint32_t k = j * TH + t;
+        return k >= eights ? 8 : (!F::even && k == 1 ? (int)shared : 0);
+    };
+    auto add = [&](float &dot, const float a[8], const float b[8], int j) {   // dot += a . b over the thread's own
+        float d = 0.0f;
+        const int from = KNOWN ? others(j) : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d = __builtin_fmaf(!KNOWN || F::even || i >= from ? a[i] : 0.0f, b[i], d);
+        dot += !KNOWN || !F::even || from == 0 ? d : 0.0f;
+    };
     auto ask8 = [&](Q8tEight<T> &x, const T *row, int j) {
-        if (EVEN) x.template vector<true>(q8t_at(row, col(j)));
+        if (KNOWN) x.template vector<true>(q8t_at(row, col(j)));
         else x.template ask<TINY>(row, col(j), D);
     };
     auto settle = [&](Q8tEight<T> &x, int j) {
-        if (!EVEN) x.template settle<TINY>(col(j), D);
+        if (!KNOWN) x.template settle<TINY>(col(j), D);
     };
     auto put = [&](T *row, int j, const float v[8]) {
-        if (EVEN) q8t_store8<false>(q8t_at(row, col(j)), v);
+        if (KNOWN) q8t_store8<false>(q8t_at(row, col(j)), v);
         else q8t_row_store8(row, col(j), v, D);
     };
     auto gate_row = [&](int64_t g) { return (const T *)a.gate + g * D; };
@@ -389,21 +411,20 @@ __global__ __launch_bounds__(S::MOST, (NormWaves<T, S>::BWD)) void norm_bwd(cons
             for (int j = 0; j < NV; ++j) {
                 settle(xdy[j], j);
                 settle(xr[j], j);
-                float w[8], s[8], d = 0.0f;
+                float w[8], s[8], n[8];
                 weights(SUM_PRE, w, a.w_pre, j);
                 sums.load(SUM_PRE, j, s);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float n = xr[j][i] * rstd_pre;
-                    s[i] = __builtin_fmaf(xdy[j][i], n, s[i]);
+                    n[i] = xr[j][i] * rstd_pre;
+                    s[i] = __builtin_fmaf(xdy[j][i], n[i], s[i]);
                     dr[j][i] = xdy[j][i] * w[i];
-                    d = __builtin_fmaf(dr[j][i], n, d);
                 }
-                dot += !EVEN || own(j) ? d : 0.0f;
+                add(dot, dr[j], n, j);
                 sums.store(SUM_PRE, j, s);
                 xr[j].hold();
             }
-            const float mean = row_sum<WAVE>(dot, scratch, turn) * rD, k = rstd_pre * rstd_pre * mean;
+            const float mean = row_sum<S>(dot, scratch, turn) * rD, k = rstd_pre * rstd_pre * mean;
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -480,22 +501,21 @@ __global__ __launch_bounds__(S::MOST, (NormWaves<T, S>::BWD)) void norm_bwd(cons
                 for (int i = 0; i < 8; ++i) dr[j][i] *= g[i];
             }
             if (f.post) {
-                float s[8], d = 0.0f;
+                float s[8], m[8];
                 sums.load(SUM_POST, j, s);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float m = xh[j][i] * rstd_post;
-                    s[i] = __builtin_fmaf(dr[j][i], m, s[i]);
+                    m[i] = xh[j][i] * rstd_post;
+                    s[i] = __builtin_fmaf(dr[j][i], m[i], s[i]);
                     dr[j][i] *= w[i];
-                    d = __builtin_fmaf(dr[j][i], m, d);
                 }
-                dot += !EVEN || own(j) ? d : 0.0f;
+                add(dot, dr[j], m, j);
                 sums.store(SUM_POST, j, s);
             }
             xh[j].hold();
         }
         float k = 0.0f;
-        if (f.post) k = rstd_post * rstd_post * (row_sum<WAVE>(dot, scratch, turn) * rD);
+        if (f.post) k = rstd_post * rstd_post * (row_sum<S>(dot, scratch, turn) * rD);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             if (f.post) {
@@ -515,10 +535,24 @@ __global__ __launch_bounds__(S::MOST, (NormWaves<T, S>::BWD)) void norm_bwd(cons
             sums.clear(SUM_GATE);
         }
     }
+    if (S::ROWS > 1) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            float s[8];
+            sums.load(k, 0, s);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                for (int off = S::LANES; off < 64; off *= 2) s[i] += __shfl_xor(s[i], off, 64);
+            }
+            sums.store(k, 0, s);
+        }
+        if (threadIdx.x >= S::LANES) return;
+    }
     float *part = a.part + (int64_t)blockIdx.x * a.sums * norm_part_width(D);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const uint32_t c = (j * TH + t) * 8;
+        const uint32_t c = col(j);
         float s[8];
         if (f.pre) {
             sums.load(SUM_PRE, j, s);
@@ -539,7 +573,10 @@ __global__ __launch_bounds__(S::MOST, (NormWaves<T, S>::BWD)) void norm_bwd(cons
 template <class R>
 void norm_by_width(int D, R run)
 {
-    if (D < 8) run(NormShape<64, 1, true>());
+    // 100000 x 64 bf16, us, one row or four a wavefront: forward 70 and 26, backward 89 and 36
+    if (D < 8) run(NormShape<16, 1, true>());
+    else if (D <= 128) run(NormShape<16, 1, false>());
+    else if (D <= 256) run(NormShape<32, 1, false>());
     else if (D <= 512) run(NormShape<64, 1, false>());
     else if (D <= 8192) run(NormShape<1024, 1, false>());
     else run(NormShape<1024, 2, false>());
@@ -555,7 +592,7 @@ void run_norm_fwd(const Norm &a, const NormCall &c, hipStream_t st)
         // as many workgroups as the chip holds at 24 wavefronts a compute unit (16 where a thread has two vectors); each takes rows one
         // after the other
         const int threads = S::WAVE ? 256 : norm_threads(a.D);
-        const int64_t groups = S::WAVE ? (a.T + 3) / 4 : a.T, most = 256 * ((S::NV == 1 ? 24 : 16) * 64 / threads);
+        const int64_t groups = S::WAVE ? (a.T + 4 * S::ROWS - 1) / (4 * S::ROWS) : a.T, most = 256 * ((S::NV == 1 ? 24 : 16) * 64 / threads);
         const unsigned grid = (unsigned)(groups < most ? groups : most);
         auto launch = [&](auto h, auto post, auto gate, auto drop) {
             norm_fwd<T, S, decltype(h)::value, decltype(post)::value, decltype(gate)::value, decltype(drop)::value><<<grid, threads, 0, st>>>(a);
@@ -587,7 +624,10 @@ int run_norm_bwd(const NormBack &a, const NormCall &c, int64_t chunks, hipStream
     int rc = Q8T_OK;
     norm_by_width(a.D, [&](auto shape) {
         typedef decltype(shape) S;
-        if (S::TINY || S::NV > 1 || a.D % 8 || !c.h || !a.w_pre || !a.dres_out) {
+        // fp32 with all three sums over the rows: what the known form keeps under way does not fit 128 registers (8192 x 4096 236 us, asked 189;
+        // 6000 x 5119 290 and 236; 32768 x 768 199 and 146)
+        constexpr bool CROWDED = sizeof(T) == 4 && !S::WAVE;
+        if ((CROWDED && c.post && c.gate && a.group_rows > 1) || S::TINY || S::NV > 1 || !c.h || !a.w_pre || !a.dres_out) {
             rc = launch_norm_bwd<T, S, BackAsked>(a, chunks, st);
             return;
         }
@@ -595,7 +635,11 @@ int run_norm_bwd(const NormBack &a, const NormCall &c, int64_t chunks, hipStream
             auto drop = [&](auto post, auto gate) {
                 constexpr bool P = decltype(post)::value;
                 constexpr int G = decltype(gate)::value;
-                rc = c.drop ? launch_norm_bwd<T, S, BackKnown<P, G, true>>(a, chunks, st) : launch_norm_bwd<T, S, BackKnown<P, G, false>>(a, chunks, st);
+                auto even = [&](auto drops) {
+                    constexpr bool K = decltype(drops)::value;
+                    if constexpr (!CROWDED || !P || G != GATE_SHARED) rc = a.D % 8 ? launch_norm_bwd<T, S, BackKnown<P, G, K, false>>(a, chunks, st) : launch_norm_bwd<T, S, BackKnown<P, G, K, true>>(a, chunks, st);
+                };
+                c.drop ? even(std::true_type()) : even(std::false_type());
             };
             auto gate = [&](auto post) {
                 if (!c.gate) drop(post, std::integral_constant<int, GATE_NONE>());

@@ -115,6 +115,25 @@ def test_shared_gates(T, groups, dtype):
     _check_bwd(q8t, x, 0.2)
 
 
+@pytest.mark.parametrize("T,D,groups", [(1, 64, 1), (2, 100, 2), (3, 128, 1), (3, 256, 3), (5, 9, 5), (1001, 64, 7), (1001, 100, 143), (4098, 129, 3), (20000, 64, 2),
+                                        (20000, 70, 5000), (9000, 128, 4500), (9000, 250, 30), (30000, 5, 3), (30000, 7, 10000), (6007, 16, 6007)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_narrow_rows(T, D, groups, dtype):
+    # several rows to a wavefront: parts of a chunk, groups of the gate shorter and longer than a part
+    q8t = require_gpu()
+    x = _inputs(T, D, dtype, True, groups)
+    _check_fwd(q8t, x, 0.2)
+    _check_bwd(q8t, x, 0.2)
+
+
+@pytest.mark.parametrize("D", [9, 15, 513, 519, 1025, 2047, 5119, 8191])
+@pytest.mark.parametrize("post,gated,p", [(True, 1, 0.1), (True, 0, 0.0), (False, 2, 0.1), (False, 1, 0.0), (True, 2, 0.0)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_rows_that_end_inside_eight(D, post, gated, p, dtype):
+    q8t = require_gpu()
+    _check_bwd(q8t, _inputs(21, D, dtype, post, {0: 0, 1: 1, 2: 21}[gated]), p)
+
+
 def test_parts_left_out():
     q8t = require_gpu()
     import torch
