@@ -304,13 +304,14 @@ struct BackAsked {
 };
 
 // One workgroup a chunk of rows: the column sums go to the workspace once; the tensors of the next row are asked for as soon as this
-// row's have been used, into the same registers.  6000 x 5120 bf16 with a shared gate and drop-out: 87 us, 4.8 TB/s with the 31 MB of
+// row's have been used, into the same registers (sixteen entries a thread leave no room for that: they are asked for where the row begins,
+// 1000 x 16384 bf16 114 us for 150).  6000 x 5120 bf16 with a shared gate and drop-out: 87 us, 4.8 TB/s with the 31 MB of
 // partial sums that 500 workgroups leave; fewer would not hide their loads.
 template <class T, class S, class F>
 __global__ __launch_bounds__(S::WAVE ? 64 : S::MOST, (NormWaves<T, S>::BWD)) void norm_bwd(const NormBack a)
 {
     constexpr int NV = S::NV;
-    constexpr bool WAVE = S::WAVE, TINY = S::TINY, KNOWN = F::known, WEIGHTS_KEPT = NV == 1;
+    constexpr bool WAVE = S::WAVE, TINY = S::TINY, KNOWN = F::known, WEIGHTS_KEPT = NV == 1, AHEAD = NV == 1;
     extern __shared__ float4 kept[];
     __shared__ float scratch[2][16];
     int turn = 0;
@@ -399,13 +400,14 @@ __global__ __launch_bounds__(S::WAVE ? 64 : S::MOST, (NormWaves<T, S>::BWD)) voi
             if (f.gate == GATE_ROWS) ask8(xg[j], gate_row(row), j);
         }
     };
-    if (first < last) {
+    if (AHEAD && first < last) {
         ask(first);
         if (f.h) ask_h(first);
     }
     for (int64_t row = first; row < last; ++row) {
         const int64_t base = row * D, after = min(row + 1, last - 1);   // behind the last row that one again
         float dr[NV][8], dot = 0.0f;
+        if (!AHEAD) ask(row);
         if (f.pre) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
@@ -443,7 +445,8 @@ __global__ __launch_bounds__(S::WAVE ? 64 : S::MOST, (NormWaves<T, S>::BWD)) voi
                 for (int i = 0; i < 8; ++i) dr[j][i] += xout[j][i];
             }
         }
-        ask(after);
+        if (AHEAD) ask(after);
+        else if (f.h) ask_h(row);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             float o[8];
@@ -524,7 +527,7 @@ __global__ __launch_bounds__(S::WAVE ? 64 : S::MOST, (NormWaves<T, S>::BWD)) voi
             }
             put((T *)a.dh + base, j, dr[j]);
         }
-        ask_h(after);
+        if (AHEAD) ask_h(after);
         if (f.gate == GATE_SHARED && !a.group_chunks && row + 1 == group_end) {   // a whole group inside the chunk
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
@@ -627,11 +630,11 @@ int run_norm_bwd(const NormBack &a, const NormCall &c, int64_t chunks, hipStream
         // fp32 with all three sums over the rows: what the known form keeps under way does not fit 128 registers (8192 x 4096 236 us, asked 189;
         // 6000 x 5119 290 and 236; 32768 x 768 199 and 146)
         constexpr bool CROWDED = sizeof(T) == 4 && !S::WAVE;
-        if ((CROWDED && c.post && c.gate && a.group_rows > 1) || S::TINY || S::NV > 1 || !c.h || !a.w_pre || !a.dres_out) {
+        if ((CROWDED && c.post && c.gate && a.group_rows > 1) || S::TINY || !c.h || !a.w_pre || !a.dres_out) {
             rc = launch_norm_bwd<T, S, BackAsked>(a, chunks, st);
             return;
         }
-        if constexpr (!S::TINY && S::NV == 1) {
+        if constexpr (!S::TINY) {
             auto drop = [&](auto post, auto gate) {
                 constexpr bool P = decltype(post)::value;
                 constexpr int G = decltype(gate)::value;
