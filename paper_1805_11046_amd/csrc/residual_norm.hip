@@ -55,16 +55,20 @@ __global__ __launch_bounds__(256) void clear(T *p, int64_t n)
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = (T)0.0f;
 }
 
-// Chunks of rows of the backward pass, a workgroup each: 16 wavefronts a compute unit keep enough loads in flight, and every chunk
-// costs D (2 or 3 times) partial sums, so there are no more than 2048.  Groups shorter than a chunk are taken whole (their gate's
-// gradient is final there), longer ones are cut.
+// Chunks of rows of the backward pass, a workgroup each: as many as the chip holds at 16 wavefronts a compute unit (128 registers), up to 2048,
+// because every chunk costs D (2 or 3 times) partial sums, written and read again; for the same reason chunks of fewer than four rows only
+// where there would be fewer than one a compute unit.  bf16, us, with 256, 512, 1024, 2048 chunks: 1000 x 16384 94, 116, 167, 168;
+// 6000 x 5120 89, 94, 107, 132; 8192 x 4096 93, 83, 91, 108; 8192 x 2048 81, 51, 48, 59; 2048 x 1024 24, 19, 20, 24; 32768 x 1024 249, 142, 92, 82.
+// Groups shorter than a chunk are taken whole (their gate's gradient is final there), longer ones are cut.
 struct Chunks {
     int64_t rows, per_group, count;
 };
 Chunks chunks_of(int64_t T, int D, int64_t group_rows)
 {
-    const int64_t want = 256 * 16 / (norm_threads(D) / 64), most = want < 512 ? 512 : (want > 2048 ? 2048 : want);
+    const int64_t fit = 16 / (norm_threads(D) / 64), most = 256 * (fit < 1 ? 1 : (fit > 8 ? 8 : fit));
+    const int64_t few = (T + 255) / 256;
     int64_t rows = (T + most - 1) / most;
+    if (rows < 4) rows = few < 4 ? few : 4;
     if (group_rows <= rows) {
         rows = (rows + group_rows - 1) / group_rows * group_rows;
         return {rows, 0, (T + rows - 1) / rows};
