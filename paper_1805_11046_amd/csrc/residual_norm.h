@@ -286,7 +286,7 @@ enum { GATE_NONE, GATE_SHARED, GATE_ROWS };   // a row of the gate for several r
 // become one for the next row's, which have just been asked for.  So every thread has eight whole entries: those behind the row's end do
 // the last eight's work along with their owner; where D is no multiple of eight, the second thread's begin among the first one's, and the
 // sums over the row leave out what is another's.  Such threads are in one wavefront, so that dres may lie where dy or dres_out does.
-// Both passes over the rows and the sums, 6000 x 5120 bf16, us: conditional 125, known 94.
+// Both passes over the rows and the sums, 6000 x 5120 bf16, us, with 512 chunks: conditional 125, known 94.
 template <bool POST, int GATE, bool DROP, bool EVEN>
 struct BackKnown {
     static constexpr bool h = true, pre = true, out = true, post = POST, drop = DROP, known = true, even = EVEN;
@@ -305,8 +305,8 @@ struct BackAsked {
 
 // One workgroup a chunk of rows: the column sums go to the workspace once; the tensors of the next row are asked for as soon as this
 // row's have been used, into the same registers (sixteen entries a thread leave no room for that: they are asked for where the row begins,
-// 1000 x 16384 bf16 114 us for 150).  6000 x 5120 bf16 with a shared gate and drop-out: 87 us, 4.8 TB/s with the 31 MB of
-// partial sums that 500 workgroups leave; fewer would not hide their loads.
+// 1000 x 16384 bf16 93 us for 131).  Bound by memory: 6000 x 5120 bf16 with a shared gate
+// and drop-out 85 us, 369 MB and 15 MB of partial sums at 4.5 TB/s; 8192 x 4096 at 5 TB/s.
 template <class T, class S, class F>
 __global__ __launch_bounds__(S::WAVE ? 64 : S::MOST, (NormWaves<T, S>::BWD)) void norm_bwd(const NormBack a)
 {
