@@ -305,7 +305,7 @@ struct BackAsked {
 
 // One workgroup a chunk of rows: the column sums go to the workspace once; the tensors of the next row are asked for as soon as this
 // row's have been used, into the same registers (sixteen entries a thread leave no room for that: they are asked for where the row begins,
-// 1000 x 16384 bf16 93 us for 131).  Bound by memory: 6000 x 5120 bf16 with a shared gate
+// 1000 x 16384 bf16 114 us for 150 with 512 chunks).  Bound by memory: 6000 x 5120 bf16 with a shared gate
 // and drop-out 85 us, 369 MB and 15 MB of partial sums at 4.5 TB/s; 8192 x 4096 at 5 TB/s.
 template <class T, class S, class F>
 __global__ __launch_bounds__(S::WAVE ? 64 : S::MOST, (NormWaves<T, S>::BWD)) void norm_bwd(const NormBack a)
