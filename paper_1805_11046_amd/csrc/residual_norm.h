@@ -285,7 +285,8 @@ enum { GATE_NONE, GATE_SHARED, GATE_ROWS };   // a row of the gate for several r
 // least.  Then no load or store hangs on a condition, and the compiler can count what is under way: a wait for one row's tensors does not
 // become one for the next row's, which have just been asked for.  So every thread has eight whole entries: those behind the row's end do
 // the last eight's work along with their owner; where D is no multiple of eight, the second thread's begin among the first one's, and the
-// sums over the row leave out what is another's.  Such threads are in one wavefront, so that dres may lie where dy or dres_out does.
+// sums over the row leave out what is another's.  Such threads are in one wavefront, so that dres may lie where dy or dres_out does; with
+// two vectors a thread some are not, and such a call takes the other form.
 // Both passes over the rows and the sums, 6000 x 5120 bf16, us, with 512 chunks: conditional 125, known 94.
 template <bool POST, int GATE, bool DROP, bool EVEN>
 struct BackKnown {
@@ -630,7 +631,8 @@ int run_norm_bwd(const NormBack &a, const NormCall &c, int64_t chunks, hipStream
         // fp32 with all three sums over the rows: what the known form keeps under way does not fit 128 registers (8192 x 4096 236 us, asked 189;
         // 6000 x 5119 290 and 236; 32768 x 768 199 and 146)
         constexpr bool CROWDED = sizeof(T) == 4 && !S::WAVE;
-        if ((CROWDED && c.post && c.gate && a.group_rows > 1) || S::TINY || !c.h || !a.w_pre || !a.dres_out) {
+        const bool over = S::NV > 1 && (a.dres == a.dy || a.dres == a.dres_out);
+        if (over || (CROWDED && c.post && c.gate && a.group_rows > 1) || S::TINY || !c.h || !a.w_pre || !a.dres_out) {
             rc = launch_norm_bwd<T, S, BackAsked>(a, chunks, st);
             return;
         }

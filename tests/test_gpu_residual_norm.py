@@ -252,6 +252,33 @@ def test_in_place_through_the_c_calls():
         assert torch.equal(t[into], grads[0]) and torch.equal(dh, grads[1]) and torch.equal(wp, grads[3]) and torch.equal(wq, grads[4])
 
 
+@pytest.mark.parametrize("D", [9, 100, 515, 4100, 5120, 8200, 12290, 16384])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_gradient_over_an_input_through_the_c_call(D, dtype):
+    q8t = require_gpu()
+    import torch
+    L = q8t.binding._lib
+    T, dt = 40, getattr(torch, dtype)
+    x = _inputs(T, D, dtype, True, 1)
+    fwd = q8t.residual_norm_fwd(x["res"], x["h"], w_post=x["w_post"], gate=x["gate"], w_pre=x["w_pre"], p=0.1, seed=3)
+    H, s = {k: plain.host(v) for k, v in x.items()}, plain.host(fwd[2])
+    keep = plain.kept(T * D, 0.1, 3).reshape(T, D)
+    ins = (H["dy"], H["dres_out"], plain.host(fwd[0]), H["h"], s[0], s[1], H["w_post"], H["gate"], H["w_pre"], 1.0, 1.0, keep)
+    want, size = plain.norm_bwd(*ins), plain.norm_bwd(*ins, size=True)
+    p = lambda t: t.data_ptr()   # noqa: E731
+    for into in ("dy", "dres_out"):
+        t = {k: x[k].clone() for k in ("dy", "dres_out")}
+        dh, dg = torch.empty_like(x["h"]), torch.empty_like(x["gate"])
+        wp, wq = torch.empty(D, device="cuda:0"), torch.empty(D, device="cuda:0")
+        ws = torch.empty(L.q8t_residual_norm_bwd_workspace_size(T, D, 1), dtype=torch.uint8, device="cuda:0")
+        assert L.q8t_residual_norm_bwd(p(t["dy"]), p(t["dres_out"]), p(fwd[0]), p(x["h"]), p(fwd[2]), p(x["w_post"]), p(x["gate"]), 1, p(x["w_pre"]),
+                                       int(dt == torch.bfloat16), T, D, 1.0, 1.0, 0.1, 3, None, p(t[into]), p(dh), p(dg), p(wp), p(wq), p(ws),
+                                       torch.cuda.current_stream().cuda_stream) == 0
+        for name, g, w, z in zip(("dres", "dh", "dgate", "dw_post", "dw_pre"), (t[into], dh, dg, wp, wq), want, size):
+            rows = T if name[:2] == "dw" or name == "dgate" else 0           # as in _check_bwd
+            plain.within(g, w, plain.HALF[g.dtype] * np.abs(w) + (128 + rows) * U * z, name)
+
+
 def test_beyond_32_bits():
     q8t = require_gpu()
     import torch
