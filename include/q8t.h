@@ -466,8 +466,8 @@ int q8t_fp8_quantize(const void *x, int type, int64_t rows, int64_t cols, int fo
                      const int64_t *step, uint8_t *q, uint8_t *s, uint8_t *qt, uint8_t *st, void *stream);
 
 /* out[m][n] = sum_k A[m][k] B[n][k] over codes as q8t_fp8_quantize leaves them: a [M][128*ceil(K/128)], sa [M][4*ceil(K/512)], b and sb
- * likewise with N rows.  A fp32 result is summed in fp32; for a bf16 result the products are added in groups of eight, where what lies
- * below 2^-13 of the group's largest product is lost, and the groups in fp32.  What a code and its scale stand for has to be within
+ * likewise with N rows.  A fp32 result is summed in fp32; for a bf16 result of more than a few rows the products are added in groups of
+ * eight, where what lies below 2^-13 of the group's largest product is lost, and the groups in fp32.  What a code and its scale stand for has to be within
  * the range of fp32, as it is where it came from there.  The three products of a layer Y[M,N] = X[M,K] W[K,N]:
  *   forward          a = q of X,  b = qt of W          layer gradient   a = q of dY,  b = q of W
  *   weight gradient  a = qt of X, b = qt of dY

@@ -1,14 +1,16 @@
 // Products of 8-bit floating point codes with a scale for each block of 128 of the reduction: out[m][n] = sum_k A[m][k] B[n][k].
 //
-// Two ways to multiply, by the type of the result:
-//   bf16: the 8-bit matrix instruction over 128 entries, which takes the scales as operands, a byte (exponent + 127) for every row of
+// Two ways to multiply:
+//   codes: the 8-bit matrix instruction over 128 entries, which takes the scales as operands, a byte (exponent + 127) for every row of
 //     either operand: a block of 128 is one instruction and its scaling costs nothing.  Inside, it adds products in groups of eight
 //     and there loses what lies below 2^-13 of the group's largest (measured: 1 + 2^-13 is kept, 1 + 2^-14 is 1; over random operands
-//     the result is 0.8e-5 to 1.5e-5 off in the 2-norm), the sums of groups are fp32.  A bf16 result is off by up to 2^-8 anyway.
-//   fp32: codes become bf16 values with their scale already on, two in an instruction and exactly (a code has at most four
-//     significant bits, and what they stand for came out of a fp32 value), and the bf16 matrix instruction adds them in fp32
-//     (2e-8 off).  Half the rate of the 8-bit one, which such results need: every fp8 instruction of this chip, with scales or
-//     without, adds in the same groups.
+//     the result is 0.8e-5 to 1.5e-5 off in the 2-norm), the sums of groups are fp32.
+//   values: codes become bf16 values with their scale already on, two in an instruction (a code has at most four significant bits, so
+//     this is exact within bf16's range), and the bf16 matrix instruction adds them in fp32 (2e-8 off).  Half the rate of the other:
+//     every fp8 instruction of this chip, with scales or without, adds in the same groups.
+// Results in fp32 are products of values.  Results in bf16, which are off by up to 2^-8 anyway, are products of codes in the tiles, where
+// the matrix instructions' rate counts (2048 x 4096 x 4096 in 36 us, of values 58), and of values with few rows, where it does not (one
+// row by 4096 x 4096 4.8 us either way, 32 rows 8.3, 64 rows 10.4 and 10.5), but for blocks with scales beyond bf16's range.
 // Both operands are read with one assignment of a lane's registers to positions inside a block; which it is does not matter to a
 // sum over the block.  Rows are whole blocks (filled up with zeros), so the reduction has no tail; rows behind the last are read
 // as the last one and not stored: a row of the result depends on its own row of A and its own row of B alone.
@@ -88,6 +90,10 @@ struct Part<FMT, true> {
     }
 };
 
+// Whether a stored scale may bring codes out of bf16's range: below its last place, 2^-133, or to 2^128 (e5m2's least code is 2^-16, its
+// largest 1.75 * 2^15; e4m3's lie between), or stands for NaN.
+__device__ __forceinline__ bool beyond_bf16(uint32_t scale) { return scale - 10u > 229u; }
+
 // D[i][j] += sum over the block of P[i][.] Q[j][.]; lane l holds entries of rows l % 16 of both and D[4 * (l / 16) + 0..3][l % 16]
 template <int BYTE, int FP, int FQ>
 __device__ __forceinline__ f32x4 block_product(const Part<FP, false> &p, const Part<FQ, false> &q, f32x4 acc)
@@ -112,12 +118,12 @@ __device__ __forceinline__ void store4(OUT *out, int64_t at, const f32x4 v, int 
 }
 
 // Operands straight from memory to registers; the W wavefronts of a workgroup share a tile of 16*MT x 16*NT results and take turns at
-// the reduction, four blocks at a time, because four scales of a row are one word.  Bound by the weights' bytes: one row by 4096 x 4096 in
+// the reduction, four blocks at a time, because four scales of a row are one word.  Products of values (for bf16 results, a block under a
+// scale beyond bf16's range as codes).  Bound by the weights' bytes: one row by 4096 x 4096 in
 // 4.4 us, by 8192 x 8192 in 12.4 (5.5 TB/s).
 template <int FA, int FB, class OUT, int MT, int NT, int W>
 __global__ __launch_bounds__(64 * W) void direct(const Product p)
 {
-    constexpr bool WIDE = std::is_same<OUT, float>::value;
     __shared__ f32x4 fold[W > 1 ? W : 1][MT * NT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, r = lane & 15, g = lane / 16;
     const int n0 = blockIdx.x * (16 * NT), m0 = blockIdx.y * (16 * MT);
@@ -150,18 +156,38 @@ __global__ __launch_bounds__(64 * W) void direct(const Product p)
             constexpr int B = decltype(byte)::value;
             if (k0 + B >= p.nk) return;
             const int64_t at = (int64_t)(k0 + B) * 128;
-            Part<FA, WIDE> a[MT];
-            Part<FB, WIDE> b[NT];
+            i32x4 ca[MT][2], cb[NT][2];
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-                a[i].template set<B>(*reinterpret_cast<const i32x4 *>(pa[i] + at), *reinterpret_cast<const i32x4 *>(pa[i] + at + 64), sa[i]);
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-                b[j].template set<B>(*reinterpret_cast<const i32x4 *>(pb[j] + at), *reinterpret_cast<const i32x4 *>(pb[j] + at + 64), sb[j]);
+                for (int i = 0; i < MT; ++i) ca[i][h] = *reinterpret_cast<const i32x4 *>(pa[i] + at + 64 * h);
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+                for (int j = 0; j < NT; ++j) cb[j][h] = *reinterpret_cast<const i32x4 *>(pb[j] + at + 64 * h);
+            }
+            auto add = [&](auto wide) {
+                constexpr bool WIDE = decltype(wide)::value;
+                Part<FA, WIDE> a[MT];
+                Part<FB, WIDE> b[NT];
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = block_product<B>(b[j], a[i], acc[i][j]);
+                for (int i = 0; i < MT; ++i) a[i].template set<B>(ca[i][0], ca[i][1], sa[i]);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) b[j].template set<B>(cb[j][0], cb[j][1], sb[j]);
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = block_product<B>(b[j], a[i], acc[i][j]);
+            };
+            if (std::is_same<OUT, float>::value) {
+                add(std::true_type());
+                return;
+            }
+            bool far = false;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) far = far || beyond_bf16(((uint32_t)sa[i] >> (8 * B)) & 255u);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) far = far || beyond_bf16(((uint32_t)sb[j] >> (8 * B)) & 255u);
+            if (__any(far)) add(std::false_type());
+            else add(std::true_type());
         };
         step(std::integral_constant<int, 0>());
         step(std::integral_constant<int, 1>());

@@ -1,0 +1,67 @@
+"""What a product of 8-bit floating point codes keeps of its sums: small terms beside large ones that cancel."""
+import numpy as np
+import pytest
+
+import lm_plain as plain
+from gpu_util import require_gpu
+
+pytestmark = pytest.mark.gpu
+
+# products of few rows, which read their operands straight to registers
+FEW = [(1, 4093, 4100), (13, 300, 1030), (29, 4090, 4000), (61, 515, 2000), (61, 4090, 4000)]
+
+
+def _device(q, s, fmt):
+    import torch
+    code = torch.float8_e4m3fn if fmt == "e4m3" else torch.float8_e5m2
+    return torch.from_numpy(q).to(torch.float32).to(code).to("cuda:0"), torch.from_numpy(s).to("cuda:0").view(torch.float8_e8m0fnu)
+
+
+def _cancelling(M, N, K, fa, fb):
+    """Codes and scales on the device, and the exact product: in each block 1 and -1, and 2^-16 or -2^-16 for every other entry.  All sums are
+    whole numbers of 2^-16 below 2^7, exact in fp32 in any order."""
+    g = np.random.default_rng(M + N + K)
+    nb = K // 128
+    Kp = -(-K // 128) * 128
+    a, b = np.zeros((M, Kp)), np.zeros((N, Kp))
+    a[:, :K] = g.choice([-1.0, 1.0], (M, K)) * 2.0 ** -8
+    b[:, :K] = g.choice([-1.0, 1.0], (N, K)) * 2.0 ** -8
+    sign = g.choice([-1.0, 1.0], (M, nb))
+    for k in range(nb):
+        at = 128 * k + g.choice(128, 2, replace=False)
+        a[:, at] = sign[:, k, None] * np.array([1.0, -1.0])
+        b[:, at] = 1.0
+    ones = [np.full((R, -(-Kp // 512) * 4), 127, np.uint8) for R in (M, N)]
+    want = (a.astype(np.float32) * np.float32(2 ** 8)) @ (b.astype(np.float32) * np.float32(2 ** 8)).T * np.float32(2.0 ** -16)
+    assert np.abs(want).max() < 128
+    return _device(a, ones[0], fa) + _device(b, ones[1], fb), want
+
+
+@pytest.mark.parametrize("M,N,K", FEW)
+@pytest.mark.parametrize("fa,fb", [("e4m3", "e4m3"), ("e4m3", "e5m2"), ("e5m2", "e4m3")])
+def test_few_rows_to_bf16_are_summed_in_fp32(M, N, K, fa, fb):
+    q8t = require_gpu()
+    import torch
+    ops, want = _cancelling(M, N, K, fa, fb)
+    assert torch.equal(q8t.fp8_gemm(*ops).cpu(), torch.from_numpy(want).bfloat16())
+
+
+@pytest.mark.parametrize("M,N,K", FEW + [(20, 30, 256)])
+def test_few_rows_to_bf16_at_the_ends_of_the_scales(M, N, K):
+    # what codes and scales stand for: below bf16's last place, 2^-133, or above its largest number, next to rows of ordinary scales
+    q8t = require_gpu()
+    K = K // 128 * 128
+    for code, ea, eb in ((2.0 ** -9, 0, 254), (1.0, 0, 254), (448.0, 247, 7), (448.0, 254, 0), (2.0 ** -9, 3, 251), (416.0, 240, 14)):
+        a, b = np.full((M, K), code), np.full((N, K), 1.0)
+        sa, sb = np.full((M, -(-K // 512) * 4), 127, np.uint8), np.full((N, -(-K // 512) * 4), 127, np.uint8)
+        sa[M // 2:, :K // 128] = ea
+        sb[N // 2:, :K // 128] = eb
+        want = np.full((M, N), code * K)
+        scale = np.exp2(sa[:, :1].astype(np.float64) - 127) * np.exp2(sb[:, :1].astype(np.float64).T - 127)
+        want = want * scale
+        got = plain.host(q8t.fp8_gemm(*(_device(a, sa, "e4m3") + _device(b, sb, "e5m2"))))
+        normal = (want >= 2.0 ** -126) & (want < 2.0 ** 128)
+        assert normal[M // 2:, N // 2:].all()
+        # whole multiples of one product in fp32: below 2^24 of them exact; one rounding to bf16
+        off = 2.0 ** -8 * want
+        assert (np.abs(got - want)[normal] <= off[normal]).all(), (code, ea, eb)
