@@ -203,6 +203,10 @@ __global__ __launch_bounds__(S::WAVE ? 256 : S::MOST, (NormWaves<T, S>::FWD)) vo
             for (int i = 0; i < 8; ++i) r[j][i] = r[j][i] * rstd * wpre[j][i];
             if (a.y) q8t_row_store8<true>((T *)a.y + base, c, r[j], D);
             if (a.q) {
+                if (D % 128) {   // behind the row's end the codes are zeros, also where 1 / rms is a NaN or infinite
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) r[j][i] = c + i < D ? r[j][i] : 0.0f;
+                }
                 const uint32_t s = fp8_scale<Q8T_E4M3>(fp8_max16(fp8_max8(r[j])));   // 16 threads hold a block
                 if (c < nb * 128) {
                     *reinterpret_cast<uint2 *>(a.q + row * nb * 128 + c) = fp8_codes8<Q8T_E4M3, false>(r[j], s, nullptr);
