@@ -483,7 +483,8 @@ int q8t_fp8_gemm(const uint8_t *a, const uint8_t *sa, int format_a, const uint8_
  *   u = h / sqrt(mean(h^2) + eps) * w_post                      the norm behind the block (w_post NULL: u = h)
  *   res_out = res_scale * res + branch_scale * drop(gate * u)   the residual stream
  *   y = res_out / sqrt(mean(res_out^2) + eps) * w_pre           the norm in front of the next block (w_pre NULL: none)
- * drop(v) = v / (1 - p) where a position is kept, else 0: see q8t_dropout for p, seed and step; p = 0 keeps everything.
+ * drop(v) = v / (1 - p) where a position is kept, else 0, whatever u and the gate hold there (w_post's norm counts all of h); it gives
+ * nothing to their gradients.  See q8t_dropout for p, seed and step; p = 0 keeps everything.
  * res, h, res_out, y [T][D] of one type; w_post, w_pre [D] floats; gate [groups][D] of the same type, row g for the rows
  * [g*T/groups, (g+1)*T/groups): 1 for a gate per channel, the number of sequences, or T for one per token (gate NULL: groups = 0,
  * no gate).  h NULL: the norm in front alone, over res (no w_post, gate, p; res_scale 1; res_out is not written).

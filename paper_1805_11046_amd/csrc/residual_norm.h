@@ -469,12 +469,16 @@ __global__ __launch_bounds__(S::WAVE ? 64 : S::MOST, (NormWaves<T, S>::BWD)) voi
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             settle(xh[j], j);
+            bool kept[8];   // a position that is not takes nothing of h and the gate, and gives nothing to their gradients
             if (f.drop) {
                 uint32_t bits[4];
                 if (D % 4 == 0) q8t_draw8<true>(base + col(j), sd, bits);
                 else q8t_draw8<false>(base + col(j), sd, bits);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) dr[j][i] = q8t_kept(bits, i, a.d.below) ? dr[j][i] * scale : 0.0f;
+                for (int i = 0; i < 8; ++i) {
+                    kept[i] = q8t_kept(bits, i, a.d.below);
+                    dr[j][i] = kept[i] ? dr[j][i] * scale : 0.0f;
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) dr[j][i] *= scale;
@@ -498,15 +502,15 @@ __global__ __launch_bounds__(S::WAVE ? 64 : S::MOST, (NormWaves<T, S>::BWD)) voi
                 if (f.gate == GATE_SHARED) {
                     sums.load(SUM_GATE, j, s);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s[i] = __builtin_fmaf(dr[j][i], o[i], s[i]);
+                    for (int i = 0; i < 8; ++i) s[i] = !f.drop || kept[i] ? __builtin_fmaf(dr[j][i], o[i], s[i]) : s[i];
                     sums.store(SUM_GATE, j, s);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] *= dr[j][i];
+                    for (int i = 0; i < 8; ++i) o[i] = !f.drop || kept[i] ? o[i] * dr[j][i] : 0.0f;
                     put((T *)a.dgate + base, j, o);
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) dr[j][i] *= g[i];
+                for (int i = 0; i < 8; ++i) dr[j][i] *= !f.drop || kept[i] ? g[i] : 0.0f;
             }
             if (f.post) {
                 float s[8], m[8];
