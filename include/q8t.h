@@ -460,7 +460,7 @@ enum { Q8T_E4M3 = 0, Q8T_E5M2 = 1 };
  * same values.
  *   q  [rows][128*ceil(cols/128)]: codes, filled up with zeros;  s  [rows][4*ceil(cols/512)]: E + 127 of each block, filled up with 127
  *   qt [cols][128*ceil(rows/128)], st [cols][4*ceil(rows/512)]: the transposed copy, nullable (both).  q, qt 16-byte aligned.
- * rows or cols may be 0 (nothing is written).  rows*cols <= 2^34, rows*ceil(cols/128) and cols*ceil(rows/128) < 2^28.
+ * rows or cols may be 0 (nothing is written).  rows*cols <= 2^34, rows*ceil(cols/128) and cols*ceil(rows/128) < 2^28 (q alone, not square: <= 2^28 - 16).
  * Errors: Q8T_ERR_SHAPE (sizes, alignment), Q8T_ERR_VALUE, Q8T_ERR_NULL, Q8T_ERR_HIP. */
 int q8t_fp8_quantize(const void *x, int type, int64_t rows, int64_t cols, int format, int square, int stochastic, uint64_t seed,
                      const int64_t *step, uint8_t *q, uint8_t *s, uint8_t *qt, uint8_t *st, void *stream);

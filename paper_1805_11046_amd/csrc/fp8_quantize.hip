@@ -332,6 +332,8 @@ extern "C" int q8t_fp8_quantize(const void *x, int type, int64_t rows, int64_t c
     const int64_t most = (int64_t)1 << 28, wide = (int64_t)1 << 31;
     if (rows >= wide || cols >= wide || rows > ((int64_t)1 << 34) / cols) return Q8T_ERR_SHAPE;
     if (rows * ((cols + 127) / 128) >= most || cols * ((rows + 127) / 128) >= most) return Q8T_ERR_SHAPE;
+    // the row copy alone: workgroups of 16 blocks, whole ones
+    if (!square && !qt && rows * ((cols + 127) / 128) > most - 16) return Q8T_ERR_SHAPE;
     if (!x || !q || !s || !qt != !st) return Q8T_ERR_NULL;
     if (!q8t_aligned(q, 16) || (qt && !q8t_aligned(qt, 16))) return Q8T_ERR_SHAPE;
     const Args a = {x, rows, cols, seed, step, q, s, qt, st, (hipStream_t)stream};
