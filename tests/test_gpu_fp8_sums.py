@@ -65,3 +65,20 @@ def test_few_rows_to_bf16_at_the_ends_of_the_scales(M, N, K):
         # whole multiples of one product in fp32: below 2^24 of them exact; one rounding to bf16
         off = 2.0 ** -8 * want
         assert (np.abs(got - want)[normal] <= off[normal]).all(), (code, ea, eb)
+
+
+# fp32 results: operands straight to registers, tiles of 64 x 64 in one slice and in several, and larger ones
+WIDE = [(1, 4093, 4100), (61, 4090, 4000), (250, 500, 1500), (70, 300, 8192), (500, 4090, 4000), (2000, 2100, 1500), (4090, 8200, 2000)]
+
+
+@pytest.mark.parametrize("M,N,K", WIDE)
+def test_fp32_results_at_the_ends_of_the_range_of_codes(M, N, K):
+    # 2^-133 and the largest numbers below 2^128 on one side, brought back by the other side's scale: whole multiples of one product
+    q8t = require_gpu()
+    import torch
+    K = K // 128 * 128
+    for fa, code, ea, eb in (("e4m3", 2.0 ** -9, 3, 240), ("e4m3", 448.0, 246, 9), ("e5m2", 2.0 ** -16, 10, 240), ("e5m2", 57344.0, 239, 9)):
+        a, b = np.full((M, K), code), np.full((N, K), 1.0)
+        sa, sb = np.full((M, -(-K // 512) * 4), ea, np.uint8), np.full((N, -(-K // 512) * 4), eb, np.uint8)
+        got = q8t.fp8_gemm(*(_device(a, sa, fa) + _device(b, sb, "e4m3")), dtype=torch.float32)
+        assert bool((got == code * K * 2.0 ** (ea + eb - 254)).all()), (fa, code)
