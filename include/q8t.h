@@ -442,10 +442,10 @@ int q8t_relu_bwd_sum_lattice(const float *g1, const float *g2s, const float *out
  * far larger than the others, so one range a tensor is too coarse for them; codes are 8-bit floating point there, with a scale
  * for every 128 entries along the axis that a product sums over, and the normalization runs along a token's row.
  *
- * Types of float tensors: Q8T_F32, Q8T_BF16.  All arithmetic is fp32 and a result is rounded to its type once.  Row-major,
- * contiguous; any alignment of the type itself.  step (nullable): a device counter that is added to the seed, so that a
- * captured graph draws anew at every replay.  Q8T_ERR_VALUE: a type, format or factor outside the allowed ones.  Outputs may
- * not overlap inputs unless it is said below. */
+ * Types of float tensors: Q8T_F32, Q8T_BF16.  Arithmetic is fp32, but for products to Q8T_BF16 (see there), and a result is rounded
+ * to its type once.  Row-major, contiguous; any alignment of the type itself.  step (nullable): a device counter that is added to the
+ * seed, so that a captured graph draws anew at every replay.  Q8T_ERR_VALUE: a type, format or factor outside the allowed ones.
+ * Outputs may not overlap inputs unless it is said below. */
 enum { Q8T_F32 = 0, Q8T_BF16 = 1 };
 enum { Q8T_E4M3 = 0, Q8T_E5M2 = 1 };
 

@@ -622,6 +622,7 @@ def relu_bwd_add(g, out, other=None):
 # ------------------------------------------------------------------ the 8-bit layer step of a language model
 # float tensors of float32 or bfloat16, contiguous, all of a call on one device; the call runs there, on that device's current stream.
 # step: None, or a device tensor of one int64 that is added to the seed (a captured graph then draws anew at every replay).
+# As in the rest of the library no call records a gradient: the backward pass is a call of its own.
 _FORMATS = {"e4m3": 0, "e5m2": 1}
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
@@ -642,8 +643,10 @@ def fp8_quantize(x, fmt="e4m3", square=False, stochastic=False, seed=0, step=Non
 
 
 def fp8_gemm(a, sa, b, sb, dtype=torch.bfloat16, out=None, ws=None):
-    """[M, N] = A [M, K] B [N, K]^T over codes and scales of fp8_quantize, sums in fp32; dtype: float32 or bfloat16.  With Y = X W:
-    forward (q of X, qt of W), layer gradient (q of dY, q of W), weight gradient (qt of X, qt of dY)."""
+    """[M, N] = A [M, K] B [N, K]^T over codes and scales of fp8_quantize.  dtype: float32, with sums in fp32 (for codes that stand for
+    2^-133 to 2^128), or bfloat16, where products of more than a few rows are added in groups of eight that lose what lies below 2^-13
+    of the group's largest, some 1e-5 of the result (a bfloat16 result of fp32 sums: float32, then rounded).  With Y = X W: forward
+    (q of X, qt of W), layer gradient (q of dY, q of W), weight gradient (qt of X, qt of dY)."""
     return _calls.fp8_gemm(a, sa, b, sb, _one_of(_TYPES, dtype, "dtype"), out, ws)
 
 
