@@ -18,6 +18,7 @@
 #include <type_traits>
 
 #include "fp8_codes.h"
+#include "fp8_plan.h"
 #include "gemm_core.h"
 
 struct Fp8Product {
@@ -27,12 +28,6 @@ struct Fp8Product {
     void *out;
 };
 
-// Form of a product: which kernel, and into how many slices the reduction is cut (partial sums in the workspace where there are several)
-enum Fp8Form { FP8_DIRECT_16, FP8_DIRECT_32, FP8_DIRECT_64, FP8_TILE_64, FP8_TILE_64_128, FP8_TILE_128_DEEP, FP8_TILE_128, FP8_TILE_256 };
-struct Fp8Plan {
-    Fp8Form form;
-    int slices;
-};
 // fp8_gemm_bf16.hip, fp8_gemm_f32.hip: the product with results of that type; ws: fp32 [slices][M][N] where there are several
 int q8t_fp8_product_bf16(const Fp8Product &p, int fa, int fb, const Fp8Plan &plan, void *ws, hipStream_t st);
 int q8t_fp8_product_f32(const Fp8Product &p, int fa, int fb, const Fp8Plan &plan, void *ws, hipStream_t st);
