@@ -112,14 +112,16 @@ __device__ __forceinline__ void store4(OUT *out, int64_t at, const f32x4 v, int 
         if (i < count) out[at + i] = (OUT)v[i];
 }
 
-// Operands straight from memory to registers; the W wavefronts of a workgroup share a tile of 16*MT x 16*NT results and take turns at
+// Operands straight from memory to registers; the wavefronts of a workgroup share a tile of 16*MT x 16*NT results and take turns at
 // the reduction, four blocks at a time, because four scales of a row are one word.  Products of values (for bf16 results, a block under a
 // scale beyond bf16's range as codes).  Bound by the weights' bytes: one row by 4096 x 4096 in
 // 4.4 us, by 8192 x 8192 in 12.4 (5.5 TB/s).
-template <int FA, int FB, class OUT, int MT, int NT, int W>
-__global__ __launch_bounds__(64 * W) void direct(const Product p)
+constexpr int kDirectWaves = 8;
+template <int FA, int FB, class OUT, int MT, int NT>
+__global__ __launch_bounds__(64 * kDirectWaves) void direct(const Product p)
 {
-    __shared__ f32x4 fold[W > 1 ? W : 1][MT * NT][64];
+    constexpr int W = kDirectWaves;
+    __shared__ f32x4 fold[W][MT * NT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, r = lane & 15, g = lane / 16;
     const int n0 = blockIdx.x * (16 * NT), m0 = blockIdx.y * (16 * MT);
     const uint8_t *pa[MT], *psa[MT], *pb[NT], *psb[NT];
@@ -189,24 +191,19 @@ __global__ __launch_bounds__(64 * W) void direct(const Product p)
         step(std::integral_constant<int, 2>());
         step(std::integral_constant<int, 3>());
     }
-    if (W > 1) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) fold[wave][i * NT + j][lane] = acc[i][j];
-        __syncthreads();
-    }
+        for (int j = 0; j < NT; ++j) fold[wave][i * NT + j][lane] = acc[i][j];
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             if ((i * NT + j) % W != wave) continue;   // the tiles are dealt out to the wavefronts
-            f32x4 v = acc[i][j];
-            if (W > 1) {
-                v = fold[0][i * NT + j][lane];
+            f32x4 v = fold[0][i * NT + j][lane];
 #pragma unroll
-                for (int w = 1; w < W; ++w) v += fold[w][i * NT + j][lane];
-            }
+            for (int w = 1; w < W; ++w) v += fold[w][i * NT + j][lane];
             const int m = m0 + 16 * i + r, n = n0 + 16 * j + 4 * g;
             if (m < p.M) store4((OUT *)p.out, (int64_t)m * p.N + n, v, p.N - n);
         }
@@ -521,7 +518,7 @@ int run_fold(const Product &p, int slices, const void *ws, hipStream_t st)
 template <int FA, int FB, class OUT, int MT, int NT>
 int run_direct(const Product &p, hipStream_t st)
 {
-    direct<FA, FB, OUT, MT, NT, 8><<<dim3((p.N + 16 * NT - 1) / (16 * NT), (p.M + 16 * MT - 1) / (16 * MT)), 512, 0, st>>>(p);
+    direct<FA, FB, OUT, MT, NT><<<dim3((p.N + 16 * NT - 1) / (16 * NT), (p.M + 16 * MT - 1) / (16 * MT)), 64 * kDirectWaves, 0, st>>>(p);
     Q8T_LAUNCH_CHECK();
     return Q8T_OK;
 }
