@@ -473,7 +473,8 @@ int q8t_fp8_quantize(const void *x, int type, int64_t rows, int64_t cols, int fo
  *   forward          a = q of X,  b = qt of W          layer gradient   a = q of dY,  b = q of W
  *   weight gradient  a = qt of X, b = qt of dY
  * out: [M][N], Q8T_F32 or Q8T_BF16.  a, b 16-byte, sa, sb 4-byte aligned.  M or N may be 0 (nothing is written).
- * M, N <= 2^22, M*N <= 2^36, 1 <= K <= 2^23 (an empty reduction is refused: the caller clears what no row adds to).  ws: q8t_fp8_gemm_workspace_size(M, N, K) bytes (may be 0), 16-byte aligned.  A row whose codes or scales hold a NaN gives NaN in
+ * M, N <= 2^22, M*N <= 2^36, 1 <= K <= 2^23 (an empty reduction is refused: the caller clears what no row adds to).
+ * ws: q8t_fp8_gemm_workspace_size(M, N, K) bytes (may be 0), 16-byte aligned.  A row whose codes or scales hold a NaN gives NaN in
  * its row (column) of the result and nowhere else.
  * Errors: Q8T_ERR_SHAPE (sizes, alignment), Q8T_ERR_VALUE, Q8T_ERR_NULL, Q8T_ERR_WORKSPACE, Q8T_ERR_HIP. */
 size_t q8t_fp8_gemm_workspace_size(int M, int N, int K);

@@ -10,7 +10,8 @@
 //     every fp8 instruction of this chip, with scales or without, adds in the same groups.
 // Results in fp32 are products of values.  Results in bf16, which are off by up to 2^-8 anyway, are products of codes in the tiles, where
 // the matrix instructions' rate counts (2048 x 4096 x 4096 in 36 us, of values 58), and of values with few rows, where it does not (one
-// row by 4096 x 4096 4.8 us either way, 32 rows 8.3, 64 rows 10.4 and 10.5), but for blocks with scales beyond bf16's range.
+// row by 4096 x 4096 4.8 us of codes and 4.9 of values, 32 rows 8.3 and 8.4, 64 rows 10.4 and 10.7), but of rows with scales beyond bf16's
+// range.
 // Both operands are read with one assignment of a lane's registers to positions inside a block; which it is does not matter to a
 // sum over the block.  Rows are whole blocks (filled up with zeros), so the reduction has no tail; rows behind the last are read
 // as the last one and not stored: a row of the result depends on its own row of A and its own row of B alone.
@@ -85,9 +86,15 @@ struct Part<FMT, true> {
     }
 };
 
-// Whether a stored scale may bring codes out of bf16's range: below its last place, 2^-133, or to 2^128 (e5m2's least code is 2^-16, its
-// largest 1.75 * 2^15; e4m3's lie between), or stands for NaN.
-__device__ __forceinline__ bool beyond_bf16(uint32_t scale) { return scale - 10u > 229u; }
+// Whether one of four stored scales may bring codes out of bf16's range: below its last place, 2^-133, or to 2^128 (e5m2's least code is
+// 2^-16, its largest 1.75 * 2^15; e4m3's lie between).
+__device__ __forceinline__ bool beyond_bf16(uint32_t scales)
+{
+    bool far = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) far |= (scales >> (8 * i) & 255u) - 10u > 229u;
+    return far;
+}
 
 // D[i][j] += sum over the block of P[i][.] Q[j][.]; lane l holds entries of rows l % 16 of both and D[4 * (l / 16) + 0..3][l % 16]
 template <int BYTE, int FP, int FQ>
@@ -113,83 +120,93 @@ __device__ __forceinline__ void store4(OUT *out, int64_t at, const f32x4 v, int 
 }
 
 // Operands straight from memory to registers; the wavefronts of a workgroup share a tile of 16*MT x 16*NT results and take turns at
-// the reduction, four blocks at a time, because four scales of a row are one word.  Products of values (for bf16 results, a block under a
-// scale beyond bf16's range as codes).  Bound by the weights' bytes: one row by 4096 x 4096 in
-// 4.4 us, by 8192 x 8192 in 12.4 (5.5 TB/s).
+// the reduction, four blocks at a time, because four scales of a row are one word.  Products of values, for bf16 results
+// but of rows with scales beyond bf16's range.  Bound by the weights' bytes: one row by 4096 x 4096 in 4.4 us, by 8192 x 8192 in 12.3
+// (5.5 TB/s).
 constexpr int kDirectWaves = 8;
 template <int FA, int FB, class OUT, int MT, int NT>
-__global__ __launch_bounds__(64 * kDirectWaves) void direct(const Product p)
+__global__ __launch_bounds__(64 * kDirectWaves, (MT * NT == 1 ? 8 : 4)) void direct(const Product p)
 {
     constexpr int W = kDirectWaves;
     __shared__ f32x4 fold[W][MT * NT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, r = lane & 15, g = lane / 16;
     const int n0 = blockIdx.x * (16 * NT), m0 = blockIdx.y * (16 * MT);
-    const uint8_t *pa[MT], *psa[MT], *pb[NT], *psb[NT];
+    bool fa[MT] = {}, fb[NT] = {};
+    auto reduce = [&](auto wide, f32x4 (&acc)[MT][NT]) {
+        constexpr bool WIDE = decltype(wide)::value;
+        int row0 = r;
+        asm volatile("" : "+v"(row0));   // addresses of its own: kept from one call for another they would take registers from the first
+        const uint8_t *pa[MT], *psa[MT], *pb[NT], *psb[NT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int64_t row = min(m0 + 16 * i + r, p.M - 1);
-        pa[i] = p.a + row * p.ld + g * 16;
-        psa[i] = p.sa + row * p.lds;
-    }
+        for (int i = 0; i < MT; ++i) {
+            const int64_t row = min(m0 + 16 * i + row0, p.M - 1);
+            pa[i] = p.a + row * p.ld + g * 16;
+            psa[i] = p.sa + row * p.lds;
+        }
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int64_t row = min(n0 + 16 * j + r, p.N - 1);
-        pb[j] = p.b + row * p.ld + g * 16;
-        psb[j] = p.sb + row * p.lds;
-    }
-    f32x4 acc[MT][NT];
+        for (int j = 0; j < NT; ++j) {
+            const int64_t row = min(n0 + 16 * j + row0, p.N - 1);
+            pb[j] = p.b + row * p.ld + g * 16;
+            psb[j] = p.sb + row * p.lds;
+        }
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-    for (int k0 = wave * 4; k0 < p.nk; k0 += 4 * W) {
-        int sa[MT], sb[NT];
+            for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k0 = wave * 4; k0 < p.nk; k0 += 4 * W) {
+            int sa[MT], sb[NT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) sa[i] = *reinterpret_cast<const int *>(psa[i] + k0);
+            for (int i = 0; i < MT; ++i) sa[i] = *reinterpret_cast<const int *>(psa[i] + k0);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) sb[j] = *reinterpret_cast<const int *>(psb[j] + k0);
-        auto step = [&](auto byte) {
-            constexpr int B = decltype(byte)::value;
-            if (k0 + B >= p.nk) return;
-            const int64_t at = (int64_t)(k0 + B) * 128;
-            i32x4 ca[MT][2], cb[NT][2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int i = 0; i < MT; ++i) ca[i][h] = *reinterpret_cast<const i32x4 *>(pa[i] + at + 64 * h);
-#pragma unroll
-                for (int j = 0; j < NT; ++j) cb[j][h] = *reinterpret_cast<const i32x4 *>(pb[j] + at + 64 * h);
-            }
-            auto add = [&](auto wide) {
-                constexpr bool WIDE = decltype(wide)::value;
+            for (int j = 0; j < NT; ++j) sb[j] = *reinterpret_cast<const int *>(psb[j] + k0);
+            auto step = [&](auto byte) {
+                constexpr int B = decltype(byte)::value;
+                if (k0 + B >= p.nk) return;
+                const int64_t at = (int64_t)(k0 + B) * 128;
                 Part<FA, WIDE> a[MT];
                 Part<FB, WIDE> b[NT];
 #pragma unroll
-                for (int i = 0; i < MT; ++i) a[i].template set<B>(ca[i][0], ca[i][1], sa[i]);
+                for (int i = 0; i < MT; ++i)
+                    a[i].template set<B>(*reinterpret_cast<const i32x4 *>(pa[i] + at), *reinterpret_cast<const i32x4 *>(pa[i] + at + 64), sa[i]);
 #pragma unroll
-                for (int j = 0; j < NT; ++j) b[j].template set<B>(cb[j][0], cb[j][1], sb[j]);
+                for (int j = 0; j < NT; ++j)
+                    b[j].template set<B>(*reinterpret_cast<const i32x4 *>(pb[j] + at), *reinterpret_cast<const i32x4 *>(pb[j] + at + 64), sb[j]);
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
                     for (int j = 0; j < NT; ++j) acc[i][j] = block_product<B>(b[j], a[i], acc[i][j]);
             };
-            if (std::is_same<OUT, float>::value) {
-                add(std::true_type());
-                return;
+            step(std::integral_constant<int, 0>());
+            step(std::integral_constant<int, 1>());
+            step(std::integral_constant<int, 2>());
+            step(std::integral_constant<int, 3>());
+            if (!WIDE || std::is_same<OUT, float>::value) continue;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) fa[i] |= beyond_bf16(sa[i]);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) fb[j] |= beyond_bf16(sb[j]);
+        }
+    };
+    f32x4 acc[MT][NT];
+    reduce(std::true_type(), acc);
+    if (!std::is_same<OUT, float>::value) {   // rows with such scales once more, as codes; the others' results are their own
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) any |= fa[i];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) any |= fb[j];
+        if (__any(any)) {
+            f32x4 far[MT][NT];
+            reduce(std::false_type(), far);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const uint32_t rows = (uint32_t)__ballot(fb[j]) >> (4 * g);   // bit e: of row 4 * g + e
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = fa[i] || (rows >> e & 1u) ? far[i][j][e] : acc[i][j][e];
             }
-            bool far = false;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) far = far || beyond_bf16(((uint32_t)sa[i] >> (8 * B)) & 255u);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) far = far || beyond_bf16(((uint32_t)sb[j] >> (8 * B)) & 255u);
-            if (__any(far)) add(std::false_type());
-            else add(std::true_type());
-        };
-        step(std::integral_constant<int, 0>());
-        step(std::integral_constant<int, 1>());
-        step(std::integral_constant<int, 2>());
-        step(std::integral_constant<int, 3>());
+        }
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i)

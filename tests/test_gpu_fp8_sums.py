@@ -68,6 +68,24 @@ def test_few_rows_to_bf16_at_the_ends_of_the_scales(M, N, K):
         assert (np.abs(got - want)[normal] <= off[normal]).all(), (code, ea, eb)
 
 
+@pytest.mark.parametrize("M,N,K", FEW)
+@pytest.mark.parametrize("scale", [0, 3, 250, 255])
+def test_scales_at_the_ends_leave_other_rows_alone(M, N, K, scale):
+    # ordinary rows beside a row whose scales are at an end, or stand for NaN, in some blocks: the same bits as without it
+    q8t = require_gpu()
+    import torch
+    g = np.random.default_rng(K)
+    (a, sa, _, _), (b, sb, _, _) = (q8t.fp8_quantize(torch.from_numpy(g.standard_normal((R, K), np.float32)).to("cuda:0"), f) for R, f in ((M, "e4m3"), (N, "e5m2")))
+    want = q8t.fp8_gemm(a, sa, b, sb)
+    rows, cols = torch.arange(M) % 5 != 2, torch.arange(N) % 7 != 3
+    sa.view(torch.uint8)[~rows, 1:8:2] = scale
+    sb.view(torch.uint8)[~cols, 2:7] = scale
+    got = q8t.fp8_gemm(a, sa, b, sb)
+    assert torch.equal(got[rows][:, cols], want[rows][:, cols])
+    if scale == 255:
+        assert bool(got[~rows].isnan().all()) and bool(got[:, ~cols].isnan().all())
+
+
 # fp32 results: operands straight to registers, tiles of 64 x 64 in one slice and in several, and larger ones
 WIDE = [(1, 4093, 4100), (61, 4090, 4000), (250, 500, 1500), (70, 300, 8192), (500, 4090, 4000), (2000, 2100, 1500), (4090, 8200, 2000)]
 
