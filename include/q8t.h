@@ -466,10 +466,11 @@ int q8t_fp8_quantize(const void *x, int type, int64_t rows, int64_t cols, int fo
                      const int64_t *step, uint8_t *q, uint8_t *s, uint8_t *qt, uint8_t *st, void *stream);
 
 /* out[m][n] = sum_k A[m][k] B[n][k] over codes as q8t_fp8_quantize leaves them: a [M][128*ceil(K/128)], sa [M][4*ceil(K/512)], b and sb
- * likewise with N rows.  A fp32 result is summed in fp32; for a bf16 result of more than a few rows the products are added in groups of
- * eight, where what lies below 2^-13 of the group's largest product is lost, and the groups in fp32.  For a fp32 result
+ * likewise with N rows.  A fp32 result is summed in fp32; for a bf16 result the products may be added in groups of eight, where what lies
+ * below 2^-13 of the group's largest product is lost, and the groups in fp32 (as a rule with more than 64 rows).  For a fp32 result
  * what a code and its scale stand for is 0 or between 2^-133 and 2^128 in magnitude, as it is for all codes of a block whose largest
- * magnitude was between 2^-102 and 2^127: smaller ones may count as 0, larger ones as infinite.  The three products of a layer Y[M,N] = X[M,K] W[K,N]:
+ * magnitude was between 2^-102 and 2^127: smaller ones may count as 0, larger ones as infinite.
+ * The three products of a layer Y[M,N] = X[M,K] W[K,N]:
  *   forward          a = q of X,  b = qt of W          layer gradient   a = q of dY,  b = q of W
  *   weight gradient  a = qt of X, b = qt of dY
  * out: [M][N], Q8T_F32 or Q8T_BF16.  a, b 16-byte, sa, sb 4-byte aligned.  M or N may be 0 (nothing is written).

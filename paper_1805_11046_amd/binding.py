@@ -644,10 +644,10 @@ def fp8_quantize(x, fmt="e4m3", square=False, stochastic=False, seed=0, step=Non
 
 def fp8_gemm(a, sa, b, sb, dtype=torch.bfloat16, out=None, ws=None):
     """[M, N] = A [M, K] B [N, K]^T over codes and scales of fp8_quantize.  dtype: float32, with sums in fp32 (for codes that stand for
-    2^-133 to 2^128), or bfloat16, where products of more than a few rows are added in groups of eight that lose what lies below 2^-13
-    of the group's largest, some 1e-5 of the result (a bfloat16 result of fp32 sums: float32, then rounded).  With Y = X W: forward
-    (q of X, qt of W), layer gradient (q of dY, q of W), weight gradient (qt of X, qt of dY).  K = 0 is refused: without rows the weight
-    gradient is the caller's zeros."""
+    2^-133 to 2^128), or bfloat16, where products may be added in groups of eight that lose what lies below 2^-13 of the group's
+    largest, some 1e-5 of the result, as a rule with more than 64 rows (bfloat16 of fp32 sums: float32, then rounded).  With Y = X W:
+    forward (q of X, qt of W), layer gradient (q of dY, q of W), weight gradient (qt of X, qt of dY).  K = 0 is refused: without rows
+    the weight gradient is the caller's zeros."""
     return _calls.fp8_gemm(a, sa, b, sb, _one_of(_TYPES, dtype, "dtype"), out, ws)
 
 

@@ -6,8 +6,8 @@
 //     and there loses what lies below 2^-13 of the group's largest (measured: 1 + 2^-13 is kept, 1 + 2^-14 is 1; over random operands
 //     the result is 0.8e-5 to 1.5e-5 off in the 2-norm), the sums of groups are fp32.
 //   values: codes become bf16 values with their scale already on, two in an instruction (a code has at most four significant bits, so
-//     this is exact from bf16's last place, 2^-133, to its largest number), and the bf16 matrix instruction adds them in fp32 (2e-8 off).  Half the rate of the other:
-//     every fp8 instruction of this chip, with scales or without, adds in the same groups.
+//     this is exact from bf16's last place, 2^-133, to its largest number), and the bf16 matrix instruction adds them in fp32 (2e-8
+//     off).  Half the rate of the other: every fp8 instruction of this chip, with scales or without, adds in the same groups.
 // Results in fp32 are products of values.  Results in bf16, which are off by up to 2^-8 anyway, are products of codes in the tiles, where
 // the matrix instructions' rate counts (2048 x 4096 x 4096 in 36 us, of values 58), and of values with few rows, where it does not (one
 // row by 4096 x 4096 4.8 us of codes and 4.9 of values, 32 rows 8.3 and 8.4, 64 rows 10.4 and 10.7), but of rows with scales beyond bf16's

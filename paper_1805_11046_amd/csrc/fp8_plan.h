@@ -67,17 +67,21 @@ Fp8Plan fp8_plan_of(int M, int N, int nk, int type)
             consider(x.f, 1, bytes / 9e6 > chain ? bytes / 9e6 : chain);
         }
     }
+    // Tiles sum a bf16 result less exactly than the direct forms; where those take all weights from memory once or run in one round, the
+    // estimates differ by less than they are off (a call in a graph, us, direct and tile 64: 1 x 100 x 300 2.6 and 2.9, 2 x 6122 x 421 3.1 and 3.3,
+    // 58 x 318 x 418 3.1 and 3.6, but 54 x 3217 x 1003 6.3 and 4.5).
+    const double worth = type == Q8T_BF16 && (M <= 16 || (M <= 64 && up(M, 16) * up(N, 16) <= kUnits)) ? 1.0 : 0.0;
     const TileCost *cost = type == Q8T_F32 ? kF32 : kBf16;
     const int n = type == Q8T_F32 ? (int)(sizeof(kF32) / sizeof(kF32[0])) : (int)(sizeof(kBf16) / sizeof(kBf16[0]));
     for (int i = 0; i < n; ++i) {
         const int64_t tiles = up(M, cost[i].bm) * up(N, cost[i].bn);
         if (tiles > 1 << 22) continue;   // a launch holds fewer than 2^32 threads
-        consider(cost[i].form, 1, tile_us(cost[i], tiles, nk));
+        consider(cost[i].form, 1, tile_us(cost[i], tiles, nk) + worth);
         // Few small tiles under a long reduction: slices of it fill the chip; their sums cost a launch and cross memory twice (512 x 512
         // x 8192 to fp32 37 us in one slice, 17 in four).
         if (cost[i].form != FP8_TILE_64 || tiles > kUnits) continue;
         for (int z = 2; z <= 16 && z * 8 <= nk; z *= 2)
-            consider(cost[i].form, z, tile_us(cost[i], tiles * z, (int)up(up(nk, z), 4) * 4) + 2.5 + (double)M * N * 4.0 * (2 * z + 1) / 4e6);
+            consider(cost[i].form, z, worth + tile_us(cost[i], tiles * z, (int)up(up(nk, z), 4) * 4) + 2.5 + (double)M * N * 4.0 * (2 * z + 1) / 4e6);
     }
     return best;
 }

@@ -49,6 +49,12 @@ def test_every_form_is_taken(plans):
     assert all(K > 8 * 128 for _, _, K, _, _ in FORMS)
 
 
+def test_small_products_of_few_rows_to_bf16_are_direct(plans):
+    # their sums are fp32; the tiles' are not
+    for case in ((1, 100, 300), (16, 48, 640), (64, 70, 130), (1, 4096, 4096), (2, 6122, 421), (58, 318, 418)):
+        assert plans(case + (1,))[0][0].startswith("direct"), case
+
+
 def test_sizes_at_the_limits_have_a_form(plans):
     big = 1 << 22
     for case in ((1, big, 128, 1), (big, 1, 128, 0), (big, 1 << 14, 128, 1), (1 << 14, big, 1 << 23, 0), (1, 1, 1 << 23, 1), (1, 1, 1, 0), (65, big, 1, 1)):

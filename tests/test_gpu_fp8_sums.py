@@ -9,7 +9,7 @@ from gpu_util import require_gpu
 pytestmark = pytest.mark.gpu
 
 # products of few rows, which read their operands straight to registers
-FEW = [(1, 4093, 4100), (13, 300, 1030), (29, 4090, 4000), (61, 515, 2000), (61, 4090, 4000)]
+FEW = [(1, 4093, 4100), (1, 100, 300), (16, 48, 640), (64, 70, 130), (13, 300, 1030), (29, 4090, 4000), (61, 515, 2000), (61, 4090, 4000)]
 
 
 def _device(q, s, fmt):
@@ -83,7 +83,7 @@ def test_scales_at_the_ends_leave_other_rows_alone(M, N, K, scale):
     got = q8t.fp8_gemm(a, sa, b, sb)
     assert torch.equal(got[rows][:, cols], want[rows][:, cols])
     if scale == 255:
-        assert bool(got[~rows].isnan().all()) and bool(got[:, ~cols].isnan().all())
+        assert bool(got[~rows].isnan().all()) and (K <= 256 or bool(got[:, ~cols].isnan().all()))    # block 2 on: behind the end of 130
 
 
 # fp32 results: operands straight to registers, tiles of 64 x 64 in one slice and in several, and larger ones
