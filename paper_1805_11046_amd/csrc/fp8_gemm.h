@@ -121,7 +121,7 @@ __device__ __forceinline__ void store4(OUT *out, int64_t at, const f32x4 v, int 
 
 // Operands straight from memory to registers; the wavefronts of a workgroup share a tile of 16*MT x 16*NT results and take turns at
 // the reduction, four blocks at a time, because four scales of a row are one word.  Products of values, for bf16 results
-// but of rows with scales beyond bf16's range.  Bound by the weights' bytes: one row by 4096 x 4096 in 4.4 us, by 8192 x 8192 in 12.3
+// but of rows with scales beyond bf16's range.  Bound by the weights' bytes: one row by 4096 x 4096 in 4.6 us, by 8192 x 8192 in 12.3
 // (5.5 TB/s).
 constexpr int kDirectWaves = 8;
 template <int FA, int FB, class OUT, int MT, int NT>
@@ -232,8 +232,9 @@ __global__ __launch_bounds__(64 * kDirectWaves, (MT * NT == 1 ? 8 : 4)) void dir
 // registers while the first part of the next step is read and the slot just read is filled with the step behind that.  Piece s of LDS
 // row r holds the 16 bytes s ^ perm(r) of the row's block, which keeps the fragment reads free of bank conflicts.  The scales of four
 // steps are a word a row and go to LDS beside them.
-// 8192 cubed: bf16 in 456 us (2.4 PFLOP/s), fp32 in 752 (1.46), tiles of 256 x 256, bound by the matrix instructions at the clock that the
-// power leaves (1.8 GHz; busy 75 % of the cycles to fp32).  2048 x 4096 x 4096 to bf16 in 34 us, tiles of 128 x 128, bound by the copies.
+// 8192 cubed: bf16 in 465 us (2.4 PFLOP/s), fp32 in 760 to 820 (1.34 to 1.45), tiles of 256 x 256, bound by the matrix instructions at the
+// clock that the power leaves (1.77 GHz; busy 75 % of the cycles to fp32).  2048 x 4096 x 4096 to bf16 in 35 to 36 us among other calls and
+// 38 to 46 on an idle card, tiles of 128 x 128, bound by the copies.
 template <int BM_, int BN_, int WM_, int WN_, int SLOTS_>
 struct Tile {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, SLOTS = SLOTS_, MT = WM / 32, NT = WN / 32;

@@ -18,8 +18,8 @@ namespace {
 //            1.3 (2.5, 5) us for every four blocks of its eighth of the reduction
 //   tiles    a step of one block takes `alone` where a compute unit has one tile and `full` for each tile where all units hold as many
 //            as fit (`fit`); a round of tiles `start` for the first copies and the last stores
-// bf16 / fp32 at 4096 x 4096 weights, us, M = 16: direct 16 6.1 / 6.1, tile 64 9.9 / 20; 32: direct 32 8.3 / 8.2; 64: direct 64 10.4 / 10.6,
-// tile 64 10.5 / 21; 128: tile 64 10.5 / 21; 512: tile 64 x 128 14.3 / 26, 128 deep 17 / -; 1024: 128 deep 21 / -, 128 27 / 33; 2048: 128 35 / 58,
+// bf16 / fp32 at 4096 x 4096 weights, us, M = 16: direct 16 6.2 / 6.1, tile 64 9.9 / 20; 32: direct 32 8.4 / 8.2; 64: direct 64 10.6 / 10.5,
+// tile 64 10.5 / 21; 128: tile 64 10.5 / 21, in four slices - / 15; 512: tile 64 x 128 14.3 / 26, 128 deep 17 / -; 1024: 128 deep 21 / -, 128 27 / 33; 2048: 128 35 / 58,
 // 256 41 / 76; 4096: 256 53 / 99, 128 68 / 113.
 struct TileCost {
     Fp8Form form;

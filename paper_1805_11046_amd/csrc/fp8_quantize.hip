@@ -116,9 +116,10 @@ __device__ __forceinline__ uint2 any8(const Q8tEight<T> &x, const uint32_t drawn
 // Both copies of a 128 x 128 tile from one read; every thread holds a patch of 8 x 8, so that it packs eight codes along
 // either axis.  SQUARE: one scale for the tile, and the transposed copy holds the same codes.
 // Bound by memory where the rounding is to nearest: both copies of 8192 x 8192 from bf16 in 51.5 us, the time of a copy of as many bytes;
-// one scale a tile of 4096 x 4096 from fp32 in 24.3 for 20.  Stochastic by the vector instructions, half of them the generator's, in
-// three groups of four for eight entries where a row starts inside a group: 3001 x 5003 from bf16 in 26.4 us, 3008 x 5008 in 23.2, for 12;
-// all tiles are on the card at once there and read, compute and write together.  8192 x 8192 takes 68.1.
+// one scale a tile of 4096 x 4096 from fp32 in 24.3 for 20.  Stochastic 3001 x 5003 from bf16 in 25 us for 12: all tiles are on the card at
+// once and read, compute and write together, so that memory (2.8 TB/s) and the vector unit (48 % of the cycles) wait for each other;
+// 8192 x 8192, where rounds of tiles overlap, takes 68.1.  Half of the instructions are the generator's, in three groups of four for
+// eight entries where a row starts inside a group (3008 x 5008 takes 2 us less).
 template <class T, int FMT, bool STOCH, bool ALIGNED, bool SQUARE>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void quantize_tile(const T *__restrict__ x, int64_t R, int64_t C, uint32_t nbr, uint32_t nbc,
                                                           uint64_t seed, const int64_t *__restrict__ step, uint8_t *__restrict__ q,

@@ -311,7 +311,7 @@ struct BackAsked {
 // One workgroup a chunk of rows: the column sums go to the workspace once; the tensors of the next row are asked for as soon as this
 // row's have been used, into the same registers (sixteen entries a thread leave no room for that: they are asked for where the row begins,
 // 1000 x 16384 bf16 114 us for 150 with 512 chunks).  Bound by memory: 6000 x 5120 bf16 with a shared gate
-// and drop-out 85 us, 369 MB and 15 MB of partial sums at 4.5 TB/s; 8192 x 4096 at 5 TB/s.
+// and drop-out 86 us, 369 MB and 15 MB of partial sums at 4.5 TB/s; 8192 x 4096 at 4.8 TB/s.
 template <class T, class S, class F>
 __global__ __launch_bounds__(S::WAVE ? 64 : S::MOST, (NormWaves<T, S>::BWD)) void norm_bwd(const NormBack a)
 {
@@ -593,7 +593,7 @@ __global__ __launch_bounds__(S::WAVE ? 64 : S::MOST, (NormWaves<T, S>::BWD)) voi
 template <class R>
 void norm_by_width(int D, R run)
 {
-    // 100000 x 64 bf16, us, one row or four a wavefront: forward 70 and 26, backward 89 and 36
+    // 100000 x 64 bf16, us, one row or four a wavefront: forward 70 and 26, backward 89 and 38
     if (D < 8) run(NormShape<16, 1, true>());
     else if (D <= 128) run(NormShape<16, 1, false>());
     else if (D <= 256) run(NormShape<32, 1, false>());
